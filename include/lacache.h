@@ -426,6 +426,132 @@ int lacache_first_layer_tokens(void* stream, const int32_t* token_ids, const int
 size_t lacache_first_layer_workspace_bytes(int64_t R, int64_t heads, int64_t H);
 
 /*
+ * The bf16 product of lacache_linear_bf16 with its epilogue: the projections
+ * around the attention and the first layer's 16-bit FFN (Sec. 3.4 keeps the
+ * first layer and every module but the FFN in 16 bits).
+ *   a        [M x K] bf16, w [N x K] bf16          (input)
+ *   bias     [N] bf16 or NULL                      (input)
+ *   residual [M x N] bf16 or NULL                  (input) may be out itself
+ *                                                  (the residual stream updated
+ *                                                  in place), else disjoint
+ *   out      [M x N] bf16                          (output)
+ * out = RNE_bf16(act(a w^T + bias) + residual), the sum of lacache_linear_bf16
+ * (fp32, the same bits) and the rest in fp32, one rounding at the end:
+ *   NONE x; RELU max(x, 0); SILU x / (1 + e^-x); GELU x (1 + erf(x / sqrt 2)) / 2
+ *   (off by at most 0.75e-7 |x| before the rounding); GELU_TANH x (1 +
+ *   tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
+ *   SWIGLU: w is [2N x K], gate rows first, and bias [2N]: silu(a w_gate^T +
+ *   b_gate) (a w_up^T + b_up), as the FFN's gate/up stage in 16 bits.
+ * Other act values: LACACHE_ERR_INVALID_ARG. SWIGLU needs N K < 2^30
+ * (LACACHE_ERR_UNSUPPORTED otherwise). A NaN is stored as 0x7FC0. No workspace.
+ */
+enum {
+  LACACHE_ACT_NONE = 0,
+  LACACHE_ACT_RELU = 1,
+  LACACHE_ACT_SILU = 2,
+  LACACHE_ACT_GELU = 3,
+  LACACHE_ACT_GELU_TANH = 4,
+  LACACHE_ACT_SWIGLU = 5
+};
+int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
+                            const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
+
+/*
+ * Paged key/value cache: the keys and values of finished tokens (the prompt,
+ * earlier blocks), and the attention of new tokens over them, for the layers
+ * whose attention is not memoized by FACache. A cache is an array of pages of
+ * `page` tokens,
+ *   k_cache, v_cache [num_pages x kv_heads x page x d]
+ * bf16 (LACACHE_KV_BF16) or e4m3 codes (LACACHE_KV_E4M3) with one fp32 scale
+ * per token and head, k_scale, v_scale [num_pages x kv_heads x page] (NULL for
+ * bf16): a head's vector is one quantization group (Eqs. 7-8, scale = max|x| /
+ * 448; a vector whose scale is 0 has codes of zeros, one that holds an infinity
+ * or a NaN gets that scale and reads as NaN). Token p of sequence s is
+ * place p mod page of page page_table[s][p / page] (page_table [S x max_pages]
+ * int32); sequences may share pages. kv_heads divides heads; query head h reads
+ * KV head h / (heads / kv_heads).
+ * Limits (LACACHE_ERR_UNSUPPORTED otherwise): d 64 or 128; page 16, 32, 64, 128
+ * or 256; heads <= 4096, S <= 4096, max_pages page <= 2^22, num_pages < 2^31, T
+ * <= 2^24, nq <= 64. Sizes that are not positive (S, T: negative) and other
+ * cache types are LACACHE_ERR_INVALID_ARG.
+ * Page numbers, positions and lengths are device data that the host cannot
+ * check; what the kernels do with values out of range is said at each call, and
+ * nothing is read or written out of bounds for them.
+ */
+enum { LACACHE_KV_BF16 = 0, LACACHE_KV_E4M3 = 1 };
+
+/*
+ * Rotates the queries and keys of T new tokens by their positions and stores
+ * keys and values in the cache.
+ *   qkv       [T x (heads + 2 kv_heads) d] bf16 (input) Q heads, K heads, V heads
+ *   seq_ids, positions [T] int32                (input) token t is token
+ *                                               positions[t] of sequence seq_ids[t]
+ *   rope_cos, rope_sin [rope_len x rope_dim/2] fp32 (input; rope_dim 0: no
+ *                                               rotation, the tables may be NULL)
+ *   q         [T x heads x d] bf16              (output) the rotated queries
+ *   k_cache, v_cache, k_scale, v_scale          (written at the tokens' places)
+ * Dimensions i < rope_dim/2 and i + rope_dim/2 are rotated as a pair, with the
+ * arithmetic of lacache_rope_scatter, the rest are copied; rope_dim is a
+ * multiple of 16, at most d (LACACHE_ERR_INVALID_ARG otherwise). Keys of an e4m3
+ * cache are quantized from the rotated fp32 value. A token whose sequence is
+ * outside [0, S), whose position is negative or at or behind max_pages page (or
+ * rope_len, with rotation), or whose page number is outside [0, num_pages) is
+ * skipped: neither its query row nor the cache is written (padded batches pass
+ * a sequence of -1). The places of a call's tokens must be distinct; of a place
+ * given twice the contents are unspecified. T == 0 launches nothing.
+ */
+int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_ids, const int32_t* positions, int64_t T,
+                         const float* rope_cos, const float* rope_sin, int64_t rope_len, int64_t rope_dim,
+                         const int32_t* page_table, int64_t S, int64_t max_pages, uint16_t* q, void* k_cache,
+                         void* v_cache, float* k_scale, float* v_scale, int64_t num_pages, int64_t page,
+                         int64_t heads, int64_t kv_heads, int64_t d, int cache_type);
+
+/*
+ * Attention of the last nq tokens of each of S sequences over the cache (which
+ * holds them too: append first). nq = 1 is the decoding of single tokens, nq =
+ * the block size a denoising step.
+ *   q        [S x nq x heads x d] bf16 (input) token t of sequence s is its token
+ *                                      seq_lens[s] - nq + t
+ *   seq_lens [S] int32                 (input) keys of each sequence, the new
+ *                                      tokens' included
+ *   o        [S x nq x heads x d] bf16 (output) softmax(scale q k^T) v
+ *   lse      [S x nq x heads] fp32 or NULL (output) the log-sum-exp of scale q
+ *                                      k^T, natural log
+ *   causal   0: every new token sees all keys of its sequence (a block of a
+ *            diffusion model); 1: those up to its own place
+ * A length below 0 counts as 0 and one above max_pages page as that. Keys on a
+ * page whose number is outside [0, num_pages) are left out. A row that sees no
+ * key (an empty sequence, a causal token before the first key), or whose scores
+ * are all -inf, gets o = 0 and lse = -inf. What lies behind a sequence's end on
+ * its last page, or a causal token's own place, does not reach the result,
+ * whatever it holds. scale must be finite and not negative.
+ * Arithmetic: exact products of bf16 (e4m3) values accumulated in fp32 (MFMA),
+ * scales applied in fp32, softmax in base 2 in fp32, P to 16 bits (two bf16
+ * terms) for the P V product, o rounded to bf16 once. A sequence's keys are
+ * cut into pieces whose sums are joined; where the cuts lie depends on the lengths of
+ * the call, so a row's last bits may differ between batches (the same inputs
+ * give the same bytes). S == 0 launches nothing. Uses the library workspace
+ * like lacache_ffn_fp8 (the same rules of order and capture).
+ */
+int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
+                            const float* k_scale, const float* v_scale, const int32_t* page_table,
+                            const int32_t* seq_lens, uint16_t* o, float* lse, int64_t S, int64_t nq, int64_t heads,
+                            int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page, int64_t max_pages,
+                            float scale, int causal, int cache_type);
+
+/* Bytes of workspace that lacache_paged_attention_ws needs on the current
+ * device (0 on bad arguments). */
+size_t lacache_paged_attention_workspace_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
+
+/* lacache_paged_attention with a caller-owned workspace of at least that size
+ * (256-byte aligned device memory, no initial contents needed). */
+int lacache_paged_attention_ws(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
+                               const float* k_scale, const float* v_scale, const int32_t* page_table,
+                               const int32_t* seq_lens, uint16_t* o, float* lse, int64_t S, int64_t nq, int64_t heads,
+                               int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page, int64_t max_pages,
+                               float scale, int causal, int cache_type, void* workspace, size_t ws_bytes);
+
+/*
  * Kernel-path policy for the GEMM stages, process-wide:
  *   0 = automatic (the skinny weight-streaming kernels for M <= 64 whose
  *       activation rows fit the gate/up kernel's LDS, over all of K (ceil(M/16)

@@ -11,7 +11,9 @@ import ctypes
 import numpy as np
 import torch
 
-from ._lib import (LACACHE_ERR_ALLOC, LACACHE_ERR_CAPTURE, LACACHE_ERR_HIP, LACACHE_ERR_INVALID_ARG,  # noqa: F401
+from ._lib import (LACACHE_ACT_GELU, LACACHE_ACT_GELU_TANH, LACACHE_ACT_NONE, LACACHE_ACT_RELU,  # noqa: F401
+                   LACACHE_ACT_SILU, LACACHE_ACT_SWIGLU, LACACHE_KV_BF16, LACACHE_KV_E4M3, LACACHE_ERR_ALLOC,
+                   LACACHE_ERR_CAPTURE, LACACHE_ERR_HIP, LACACHE_ERR_INVALID_ARG,
                    LACACHE_ERR_UNSUPPORTED, LACACHE_GRAN_GROUP, LACACHE_GRAN_TENSOR, LACACHE_GRAN_TOKEN, LACACHE_OK,
                    LacacheError, check, lib, status_string)
 
@@ -47,6 +49,29 @@ def _ptr(t, dtypes, name, shape=None, optional=False):
     if shape is not None and t.shape != shape:
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     return t.data_ptr()
+
+
+class _Stay:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *exc):
+        return False
+
+
+_STAY = _Stay()
+
+
+def _on(first, *others):
+    """The context in which a call on these tensors runs: their device current (its workspace and
+    compute units are the current device's). Tensors of several devices are refused."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors on %s and %s" % (dev, t.device))
+    if not first.is_cuda or dev.index == torch.cuda.current_device():
+        return _STAY  # (a host tensor is refused by name in _ptr)
+    return torch.cuda.device(dev)
 
 
 def lacache_quant_weights(w, w_q, w_s, group=GROUP, stream=None):
@@ -280,6 +305,20 @@ def lacache_linear_bf16(a, w, out, out_tap=None, stream=None):
         _ptr(out_tap, _F32, "out_tap", (M, N), optional=True), M, N, K), "lacache_linear_bf16")
 
 
+def lacache_linear_act_bf16(a, w, out, bias=None, residual=None, act=LACACHE_ACT_NONE, stream=None):
+    """out [M, N] bf16 = act(a [M, K] w[N, K]^T + bias [N]) + residual [M, N]; residual may be out.
+    act LACACHE_ACT_SWIGLU: w [2N, K] and bias [2N], gate rows first."""
+    M, K = a.shape
+    N = out.shape[1]
+    rows = 2 * N if act == LACACHE_ACT_SWIGLU else N
+    with _on(a, w, out, bias, residual):
+        check(lib().lacache_linear_act_bf16(
+            _stream(stream, a), _ptr(a, _BF16, "a"), _ptr(w, _BF16, "w", (rows, K)),
+            _ptr(bias, _BF16, "bias", (rows,), optional=True),
+            _ptr(residual, _BF16, "residual", (M, N), optional=True), _ptr(out, _BF16, "out", (M, N)), M, N, K, act),
+            "lacache_linear_act_bf16")
+
+
 def lacache_rope_scatter(qkv, rows, rope_cos, rope_sin, q, k, v, stream=None):
     """qkv [R, 3 heads 128] bf16 -> RoPE(Q, K) and V scattered to rows of q, k, v [heads, N, 128]."""
     R = qkv.shape[0]
@@ -304,6 +343,78 @@ def lacache_first_layer_tokens(token_ids, rows, embed, norm_w, w_qkv, rope_cos, 
         _ptr(rope_sin, _F32, "rope_sin", (N, 64)), _ptr(embed_cache, _BF16, "embed_cache", (N, H)),
         _ptr(q, _BF16, "q"), _ptr(k, _BF16, "k", (heads, N, d)), _ptr(v, _BF16, "v", (heads, N, d)), heads, N, H),
         "lacache_first_layer_tokens")
+
+
+# ---- paged key/value cache ---------------------------------------------------
+
+def _kv(k_cache, v_cache, k_scale, v_scale):
+    """The caches' pointers, their sizes [num_pages, kv_heads, page, d] and type."""
+    shape = k_cache.shape
+    if len(shape) != 4:
+        raise ValueError("k_cache: shape %s, expected [num_pages, kv_heads, page, d]" % (tuple(shape),))
+    e4m3 = k_cache.dtype in _U8
+    types = _U8 if e4m3 else _BF16
+    ks = vs = None
+    if e4m3:
+        ks, vs = _ptr(k_scale, _F32, "k_scale", shape[:3]), _ptr(v_scale, _F32, "v_scale", shape[:3])
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale belong to an e4m3 cache")
+    return (_ptr(k_cache, types, "k_cache"), _ptr(v_cache, types, "v_cache", shape), ks, vs, shape,
+            LACACHE_KV_E4M3 if e4m3 else LACACHE_KV_BF16)
+
+
+def lacache_paged_append(qkv, seq_ids, positions, rope_cos, rope_sin, page_table, q, k_cache, v_cache, k_scale=None,
+                         v_scale=None, stream=None):
+    """qkv [T, (heads + 2 kv_heads) d] bf16: rotates the queries into q [T, heads, d] and stores
+    rotated keys and values at token positions[t] of sequence seq_ids[t] ([T] int32) in the pages
+    page_table [S, max_pages] int32 names. k_cache, v_cache [num_pages, kv_heads, page, d] bf16, or
+    e4m3 with k_scale, v_scale [num_pages, kv_heads, page] fp32. rope_cos, rope_sin [rope_len,
+    rope_dim / 2] fp32, or None for no rotation."""
+    T, heads, d = q.shape
+    S, max_pages = page_table.shape
+    kc, vc, ks, vs, (num_pages, kv, page, dk), kind = _kv(k_cache, v_cache, k_scale, v_scale)
+    if dk != d:
+        raise ValueError("k_cache: vectors of %d, q of %d" % (dk, d))
+    rope_len = rope_dim = 0
+    cs = sn = None
+    if rope_cos is not None or rope_sin is not None:
+        cs = _ptr(rope_cos, _F32, "rope_cos")
+        rope_len, half = rope_cos.shape
+        rope_dim = 2 * half
+        sn = _ptr(rope_sin, _F32, "rope_sin", rope_cos.shape)
+    with _on(qkv, seq_ids, positions, rope_cos, rope_sin, page_table, q, k_cache, v_cache, k_scale, v_scale):
+        check(lib().lacache_paged_append(
+            _stream(stream, qkv), _ptr(qkv, _BF16, "qkv", (T, (heads + 2 * kv) * d)),
+            _ptr(seq_ids, _I32, "seq_ids", (T,)), _ptr(positions, _I32, "positions", (T,)), T, cs, sn, rope_len,
+            rope_dim, _ptr(page_table, _I32, "page_table"), S, max_pages, _ptr(q, _BF16, "q"), kc, vc, ks, vs,
+            num_pages, page, heads, kv, d, kind), "lacache_paged_append")
+
+
+def lacache_paged_attention(q, k_cache, v_cache, page_table, seq_lens, o, lse=None, k_scale=None, v_scale=None,
+                            scale=None, causal=False, workspace=None, stream=None):
+    """Attention of the last nq tokens of S sequences: q, o [S, nq, heads, d] bf16 over the cache
+    (lacache_paged_append), seq_lens [S] int32 keys each; lse [S, nq, heads] fp32 or None. scale is
+    1 / sqrt(d) by default. causal: a token sees the keys up to its own place, else all. workspace: a
+    uint8 tensor of lacache_paged_attention_workspace_bytes (the library's own without it)."""
+    S, nq, heads, d = q.shape
+    kc, vc, ks, vs, (num_pages, kv, page, dk), kind = _kv(k_cache, v_cache, k_scale, v_scale)
+    if dk != d:
+        raise ValueError("k_cache: vectors of %d, q of %d" % (dk, d))
+    max_pages = page_table.shape[1]
+    with _on(q, k_cache, v_cache, page_table, seq_lens, o, lse, k_scale, v_scale, workspace):
+        args = (_stream(stream, q), _ptr(q, _BF16, "q"), kc, vc, ks, vs,
+                _ptr(page_table, _I32, "page_table", (S, max_pages)), _ptr(seq_lens, _I32, "seq_lens", (S,)),
+                _ptr(o, _BF16, "o", q.shape), _ptr(lse, _F32, "lse", (S, nq, heads), optional=True), S, nq, heads, kv,
+                d, num_pages, page, max_pages, d ** -0.5 if scale is None else scale, int(bool(causal)), kind)
+        if workspace is None:
+            check(lib().lacache_paged_attention(*args), "lacache_paged_attention")
+        else:
+            check(lib().lacache_paged_attention_ws(*args, _ptr(workspace, (torch.uint8,), "workspace"),
+                                                   workspace.numel()), "lacache_paged_attention_ws")
+
+
+def lacache_paged_attention_workspace_bytes(S, nq, heads, kv_heads, d):
+    return int(lib().lacache_paged_attention_workspace_bytes(S, nq, heads, kv_heads, d))
 
 
 def lacache_set_path_policy(policy):

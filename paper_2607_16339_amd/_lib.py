@@ -18,9 +18,12 @@ LACACHE_ERR_HIP = -3
 LACACHE_ERR_ALLOC = -4
 LACACHE_ERR_CAPTURE = -5
 LACACHE_GRAN_GROUP, LACACHE_GRAN_TOKEN, LACACHE_GRAN_TENSOR = 0, 1, 2
+(LACACHE_ACT_NONE, LACACHE_ACT_RELU, LACACHE_ACT_SILU, LACACHE_ACT_GELU, LACACHE_ACT_GELU_TANH,
+ LACACHE_ACT_SWIGLU) = range(6)
+LACACHE_KV_BF16, LACACHE_KV_E4M3 = 0, 1
 
 # name -> (restype, argtypes)
-_P, _I64, _I = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
+_P, _I64, _I, _F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
 SIGNATURES = {
     "lacache_quant_weights": (_I, [_P, _P, _P, _P, _I64, _I64, _I]),
     "lacache_pack_weights": (_I, [_P, _P, _P, _I64, _I64]),
@@ -49,6 +52,12 @@ SIGNATURES = {
     "lacache_first_layer_tokens": (_I, [_P, _P, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64,
                                         _I64]),
     "lacache_first_layer_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
+    "lacache_linear_act_bf16": (_I, [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I]),
+    "lacache_paged_append": (_I, [_P, _P, _P, _P, _I64, _P, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P, _I64,
+                                  _I64, _I64, _I64, _I64, _I]),
+    "lacache_paged_attention": (_I, [_P] * 10 + [_I64] * 8 + [_F, _I, _I]),
+    "lacache_paged_attention_workspace_bytes": (ctypes.c_size_t, [_I64] * 5),
+    "lacache_paged_attention_ws": (_I, [_P] * 10 + [_I64] * 8 + [_F, _I, _I, _P, ctypes.c_size_t]),
     "lacache_set_path_policy": (_I, [_I]),
     "lacache_linear_tile": (_I, [_I64, _I64, _I64, _P]),
     "lacache_tiled_plan": (_I, [_I64, _I64, _I64, _I, _P]),

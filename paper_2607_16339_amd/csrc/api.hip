@@ -62,6 +62,13 @@ bool disjoint(std::initializer_list<Range> outs, std::initializer_list<Range> in
   return true;
 }
 
+// One output that must not overlap the inputs (no allocation).
+bool apart(Range out, std::initializer_list<Range> ins) {
+  for (const Range& b : ins)
+    if (out.hi != out.lo && b.hi != b.lo && overlap(out, b)) return false;
+  return true;
+}
+
 int check_group(int group) { return group == kGroup ? LACACHE_OK : LACACHE_ERR_UNSUPPORTED; }
 
 int check_dim(int64_t d, int64_t max) {
@@ -258,6 +265,60 @@ int ffn_core(hipStream_t st, const uint16_t* x, const uint16_t* y, const uint16_
     return LACACHE_ERR_HIP;
   RETURN_IF(run_gateup(st, path, w.xq, w.xs, wgu_q, wgu_s, w.hq, w.hs, nullptr, M, H, I, w.scratch));
   return run_down(st, path, w.hq, w.hs, wd_q, wd_s, out, nullptr, M, H, I, w.scratch);
+}
+
+// The sizes that the paged cache's calls share.
+constexpr int64_t kPagedMaxSeqs = 4096;
+constexpr int64_t kPagedMaxTokens = int64_t(1) << 22;  // of a sequence
+constexpr int64_t kPagedMaxNq = 64;
+int check_heads(int64_t heads, int64_t kv_heads, int64_t d) {
+  if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || d <= 0) return LACACHE_ERR_INVALID_ARG;
+  return heads > kAttnMaxHeads || (d != 64 && d != 128) ? LACACHE_ERR_UNSUPPORTED : LACACHE_OK;
+}
+int check_paged(int64_t S, int64_t max_pages, int64_t num_pages, int64_t page, int64_t heads, int64_t kv_heads,
+                int64_t d, int cache_type) {
+  if (cache_type != LACACHE_KV_BF16 && cache_type != LACACHE_KV_E4M3) return LACACHE_ERR_INVALID_ARG;
+  if (S < 0 || max_pages <= 0 || num_pages <= 0 || page <= 0) return LACACHE_ERR_INVALID_ARG;
+  RETURN_IF(check_heads(heads, kv_heads, d));
+  if (page < 16 || page > 256 || (page & (page - 1)) != 0 || S > kPagedMaxSeqs || max_pages > kPagedMaxTokens / page ||
+      num_pages > INT32_MAX)
+    return LACACHE_ERR_UNSUPPORTED;
+  return LACACHE_OK;
+}
+int log2_of(int64_t page) {
+  int n = 0;
+  while ((int64_t(1) << n) < page) ++n;
+  return n;
+}
+
+// The caller's arguments, checked; *a describes the call (S > 0).
+int check_attention(const uint16_t* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                    const float* v_scale, const int32_t* page_table, const int32_t* seq_lens, uint16_t* o, float* lse,
+                    int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page,
+                    int64_t max_pages, float scale, int causal, int cache_type, PagedAttn* a) {
+  RETURN_IF(check_paged(S, max_pages, num_pages, page, heads, kv_heads, d, cache_type));
+  if (nq <= 0 || causal < 0 || causal > 1 || !(scale >= 0.0f) || scale > 3.0e38f) return LACACHE_ERR_INVALID_ARG;
+  if (nq > kPagedMaxNq) return LACACHE_ERR_UNSUPPORTED;
+  if (S == 0) return LACACHE_OK;
+  const bool fp8 = cache_type == LACACHE_KV_E4M3;
+  if (!ptrs_ok({q, k_cache, v_cache, page_table, seq_lens, o}) || !opt_ptr_ok(lse)) return LACACHE_ERR_INVALID_ARG;
+  if (fp8 ? !ptrs_ok({k_scale, v_scale}) : (k_scale != nullptr || v_scale != nullptr)) return LACACHE_ERR_INVALID_ARG;
+  const size_t rows = static_cast<size_t>(S * nq * heads), places = static_cast<size_t>(num_pages) * kv_heads * page;
+  const size_t cb = places * d * (fp8 ? 1 : 2), sb = fp8 ? places * 4 : 0;
+  const Range rq = rng(q, rows * d * 2), rk = rng(k_cache, cb), rv = rng(v_cache, cb), rks = rng(k_scale, sb),
+              rvs = rng(v_scale, sb), rt = rng(page_table, S * max_pages * 4), rl = rng(seq_lens, S * 4);
+  const Range ro = rng(o, rows * d * 2), rs = rng(lse, lse ? rows * 4 : 0);
+  if (!apart(ro, {rq, rk, rv, rks, rvs, rt, rl, rs}) || !apart(rs, {rq, rk, rv, rks, rvs, rt, rl}))
+    return LACACHE_ERR_INVALID_ARG;
+  *a = PagedAttn{};
+  a->q = q, a->k_cache = k_cache, a->v_cache = v_cache, a->k_scale = k_scale, a->v_scale = v_scale;
+  a->table = page_table, a->seq_lens = seq_lens, a->o = o, a->lse = lse;
+  a->max_pages = max_pages, a->num_pages = num_pages;
+  a->S = static_cast<int>(S), a->nq = static_cast<int>(nq), a->heads = static_cast<int>(heads);
+  a->kv_heads = static_cast<int>(kv_heads), a->page_log2 = log2_of(page);
+  a->max_len = static_cast<int>(max_pages * page), a->causal = causal;
+  a->scale_log2 = scale * 1.4426950408889634f;
+  return LACACHE_OK;
 }
 
 }  // namespace
@@ -597,6 +658,25 @@ int lacache_linear_bf16(void* stream, const uint16_t* a, const uint16_t* w, uint
   return hip_status(launch_linear_bf16(static_cast<hipStream_t>(stream), a, w, out, out_tap, M, N, K));
 }
 
+int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
+                            const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {
+  if (act < LACACHE_ACT_NONE || act > LACACHE_ACT_SWIGLU) return LACACHE_ERR_INVALID_ARG;
+  RETURN_IF(check_m(M));
+  RETURN_IF(check_dim(N, kMaxN));
+  RETURN_IF(check_dim(K, kMaxN));
+  const bool glu = act == LACACHE_ACT_SWIGLU;
+  const int64_t rows = glu ? 2 * N : N;
+  // (the tiled kernel's 32-bit offsets into the pair rows)
+  if (glu && N * K >= (int64_t(1) << 30)) return LACACHE_ERR_UNSUPPORTED;
+  if (M == 0) return LACACHE_OK;
+  if (!ptrs_ok({a, w, out}) || !opt_ptr_ok(bias) || !opt_ptr_ok(residual)) return LACACHE_ERR_INVALID_ARG;
+  const size_t ob = static_cast<size_t>(M * N) * 2;
+  if (!apart(rng(out, ob), {rng(a, M * K * 2), rng(w, rows * K * 2), rng(bias, bias ? rows * 2 : 0),
+                            rng(residual, residual && residual != out ? ob : 0)}))
+    return LACACHE_ERR_INVALID_ARG;
+  return hip_status(launch_linear_act(static_cast<hipStream_t>(stream), a, w, bias, residual, out, M, N, K, act));
+}
+
 int lacache_linear_tile(int64_t M, int64_t N, int64_t K, int* tile) {
   RETURN_IF(check_m(M));
   RETURN_IF(check_dim(N, kMaxN));
@@ -693,6 +773,91 @@ int lacache_facache_attention(void* stream, const uint16_t* q, const uint16_t* k
   }
   return hip_status(launch_facache_attention(static_cast<hipStream_t>(stream), q, k, v, o, cache_m, cache_l, cache_o,
                                              lse, heads, N, c_begin, c_end, mode));
+}
+
+// ---------------------------------------------------------------------------
+// Paged key/value cache
+// ---------------------------------------------------------------------------
+
+int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_ids, const int32_t* positions, int64_t T,
+                         const float* rope_cos, const float* rope_sin, int64_t rope_len, int64_t rope_dim,
+                         const int32_t* page_table, int64_t S, int64_t max_pages, uint16_t* q, void* k_cache,
+                         void* v_cache, float* k_scale, float* v_scale, int64_t num_pages, int64_t page,
+                         int64_t heads, int64_t kv_heads, int64_t d, int cache_type) {
+  RETURN_IF(check_paged(S, max_pages, num_pages, page, heads, kv_heads, d, cache_type));
+  if (T < 0 || rope_dim < 0 || rope_dim % 16 != 0 || rope_dim > d || (rope_dim > 0 && rope_len <= 0))
+    return LACACHE_ERR_INVALID_ARG;
+  if (T > kMaxM || heads + 2 * kv_heads > kAttnMaxHeads) return LACACHE_ERR_UNSUPPORTED;
+  if (T == 0 || S == 0) return LACACHE_OK;
+  const bool fp8 = cache_type == LACACHE_KV_E4M3, rot = rope_dim > 0;
+  if (!ptrs_ok({qkv, seq_ids, positions, page_table, q, k_cache, v_cache})) return LACACHE_ERR_INVALID_ARG;
+  if (fp8 ? !ptrs_ok({k_scale, v_scale}) : (k_scale != nullptr || v_scale != nullptr)) return LACACHE_ERR_INVALID_ARG;
+  if (rot && !ptrs_ok({rope_cos, rope_sin})) return LACACHE_ERR_INVALID_ARG;
+  const int64_t max_len = max_pages * page;
+  const int64_t max_pos = rot && rope_len < max_len ? rope_len : max_len;
+  const size_t places = static_cast<size_t>(num_pages) * kv_heads * page, cb = places * d * (fp8 ? 1 : 2);
+  const size_t sb = fp8 ? places * 4 : 0, tab = rot ? static_cast<size_t>(max_pos) * (rope_dim / 2) * 4 : 0;
+  const Range in[6] = {rng(qkv, static_cast<size_t>(T) * (heads + 2 * kv_heads) * d * 2), rng(seq_ids, T * 4),
+                       rng(positions, T * 4), rng(rope_cos, tab), rng(rope_sin, tab),
+                       rng(page_table, S * max_pages * 4)};
+  const Range out[5] = {rng(q, static_cast<size_t>(T * heads * d) * 2), rng(k_cache, cb), rng(v_cache, cb),
+                        rng(k_scale, sb), rng(v_scale, sb)};
+  for (int i = 0; i < 5; ++i) {
+    if (!apart(out[i], {in[0], in[1], in[2], in[3], in[4], in[5]})) return LACACHE_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (!apart(out[i], {out[j]})) return LACACHE_ERR_INVALID_ARG;
+  }
+  PagedAppend a{};
+  a.qkv = qkv, a.seq_ids = seq_ids, a.positions = positions, a.cs = rope_cos, a.sn = rope_sin;
+  a.table = page_table, a.q = q, a.k_cache = k_cache, a.v_cache = v_cache, a.k_scale = k_scale, a.v_scale = v_scale;
+  a.max_pages = max_pages, a.num_pages = num_pages, a.S = static_cast<int>(S);
+  a.max_pos = static_cast<int>(max_pos), a.heads = static_cast<int>(heads), a.kv_heads = static_cast<int>(kv_heads);
+  a.rope_dim = static_cast<int>(rope_dim), a.page_log2 = log2_of(page);
+  return hip_status(launch_paged_append(static_cast<hipStream_t>(stream), a, T, d, fp8));
+}
+
+size_t lacache_paged_attention_workspace_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
+  if (S < 0 || S > kPagedMaxSeqs || nq <= 0 || nq > kPagedMaxNq || check_heads(heads, kv_heads, d) != LACACHE_OK)
+    return 0;
+  return paged_attention_ws_bytes(S, nq, heads, kv_heads, d);
+}
+
+int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
+                            const float* k_scale, const float* v_scale, const int32_t* page_table,
+                            const int32_t* seq_lens, uint16_t* o, float* lse, int64_t S, int64_t nq, int64_t heads,
+                            int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page, int64_t max_pages,
+                            float scale, int causal, int cache_type) {
+  PagedAttn a;
+  RETURN_IF(check_attention(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, o, lse, S, nq, heads, kv_heads,
+                            d, num_pages, page, max_pages, scale, causal, cache_type, &a));
+  if (S == 0) return LACACHE_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  void* ws = nullptr;
+  RETURN_IF(get_workspace(st, paged_attention_ws_bytes(S, nq, heads, kv_heads, d), &ws));
+  return hip_status(launch_paged_attention(st, a, d, cache_type == LACACHE_KV_E4M3, ws));
+}
+
+int lacache_paged_attention_ws(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
+                               const float* k_scale, const float* v_scale, const int32_t* page_table,
+                               const int32_t* seq_lens, uint16_t* o, float* lse, int64_t S, int64_t nq, int64_t heads,
+                               int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page, int64_t max_pages,
+                               float scale, int causal, int cache_type, void* workspace, size_t ws_bytes) {
+  PagedAttn a;
+  RETURN_IF(check_attention(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, o, lse, S, nq, heads, kv_heads,
+                            d, num_pages, page, max_pages, scale, causal, cache_type, &a));
+  if (S == 0) return LACACHE_OK;
+  const size_t need = paged_attention_ws_bytes(S, nq, heads, kv_heads, d);
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || ws_bytes < need)
+    return LACACHE_ERR_INVALID_ARG;
+  const size_t rows = static_cast<size_t>(S * nq * heads), places = static_cast<size_t>(num_pages) * kv_heads * page;
+  const bool fp8 = cache_type == LACACHE_KV_E4M3;
+  const size_t cb = places * d * (fp8 ? 1 : 2), sb = fp8 ? places * 4 : 0;
+  if (!apart(rng(workspace, need),
+             {rng(q, rows * d * 2), rng(k_cache, cb), rng(v_cache, cb), rng(k_scale, sb), rng(v_scale, sb),
+              rng(page_table, S * max_pages * 4), rng(seq_lens, S * 4), rng(o, rows * d * 2),
+              rng(lse, lse ? rows * 4 : 0)}))
+    return LACACHE_ERR_INVALID_ARG;
+  return hip_status(launch_paged_attention(static_cast<hipStream_t>(stream), a, d, fp8, workspace));
 }
 
 int lacache_set_path_policy(int policy) {

@@ -112,6 +112,10 @@ hipError_t launch_linear_bf16(hipStream_t st, const uint16_t* a, const uint16_t*
                               int64_t M, int64_t N, int64_t K);
 // The output tile of the call above: rows and columns of a workgroup.
 void linear_tile(int64_t M, int64_t N, int64_t K, int (&tile)[2]);
+// out [M x N] = act(a W^T + bias) + residual (bias, residual nullable; out may be
+// residual); act is a LACACHE_ACT_ value, SWIGLU with w [2N x K], bias [2N].
+hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
+                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
 // q, k, v rows of RoPE(y w_qkv^T) (rows [R], w_qkv [3 heads 128 x H]): the
 // bytes of launch_linear_bf16 followed by launch_rope_scatter, in one kernel.
 hipError_t launch_linear_rope(hipStream_t st, const uint16_t* y, const uint16_t* w_qkv, const int32_t* rows, int64_t R,
@@ -125,5 +129,45 @@ hipError_t launch_rope_scatter(hipStream_t st, const uint16_t* qkv, const int32_
 hipError_t launch_facache_attention(hipStream_t st, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                                     uint16_t* o, float* cm, float* cl, float* co, float* lse, int64_t heads, int64_t N,
                                     int64_t c0, int64_t c1, int mode);
+
+// Paged key/value cache: page p, KV head h, place i of a page of P = 1 <<
+// page_log2 tokens is row (p kv_heads + h) P + i of the caches ([rows x d], bf16
+// or e4m3 codes with a scale per row).
+struct PagedAppend {
+  const uint16_t* qkv;  // [T x (heads + 2 kv_heads) d]
+  const int32_t* seq_ids;
+  const int32_t* positions;
+  const float* cs;  // [rope_len x rope_dim / 2]
+  const float* sn;
+  const int32_t* table;  // [S x max_pages]
+  uint16_t* q;
+  void* k_cache;
+  void* v_cache;
+  float* k_scale;
+  float* v_scale;
+  int64_t max_pages, num_pages;
+  int S, max_pos;  // positions below max_pos have a page and a row of the tables
+  int heads, kv_heads, rope_dim, page_log2;
+};
+hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, int64_t d, bool fp8);
+
+struct PagedAttn {
+  const uint16_t* q;  // [S x nq x heads x d]
+  const void* k_cache;
+  const void* v_cache;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* table;
+  const int32_t* seq_lens;
+  uint16_t* o;
+  float* lse;
+  int64_t max_pages, num_pages;
+  int S, nq, heads, kv_heads, page_log2;
+  int max_len;  // max_pages P
+  int causal;
+  float scale_log2;
+};
+size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
+hipError_t launch_paged_attention(hipStream_t st, const PagedAttn& a, int64_t d, bool fp8, void* ws);
 
 }  // namespace lacache

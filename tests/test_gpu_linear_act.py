@@ -1,0 +1,164 @@
+"""The bf16 product with bias, activation and residual, on the GPU.
+
+The sum before the epilogue is lacache_linear_bf16's (its fp32 tap, tested
+elsewhere against 64 bits), so the epilogue is checked in 64 bits on that very
+sum. Tolerance: the output's rounding 2^-8 |ref|, and before it the fp32 steps:
+x = sum + bias (u = 2^-24 relative to |x|, which an activation of slope at most
+1.13 passes on), the activation's hardware exp2 and reciprocal with the
+rounding of its argument (|x| u + 8 u relative for SiLU's and tanh-GELU's
+exponential, whose cube adds 3 u |argument|), erf's formula (0.75e-7 |x|), SwiGLU's product
+and the residual's addition (u each)."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2607_16339_amd as lc
+from paged_util import DEV, normal
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+NONE, RELU, SILU, GELU, GELU_TANH, SWIGLU = range(6)
+
+
+def _act(act, x):
+    """(value, its tolerance) of the activation of x, which is off by u |x|."""
+    slack = 1.2 * U * x.abs()
+    if act == RELU:
+        return x.clamp_min(0.0), slack
+    if act in (SILU, SWIGLU):
+        y = x * torch.sigmoid(x)
+        return y, slack + y.abs() * (3 * x.abs() + 8) * U
+    if act == GELU:
+        return 0.5 * x * torch.erfc(-x / math.sqrt(2.0)), slack + x.abs() * (0.75e-7 + 8 * U)
+    if act == GELU_TANH:
+        w = 2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)
+        y = x * torch.sigmoid(w)
+        return y, slack + y.abs() * (5 * w.abs() + 8) * U
+    return x, slack
+
+
+def _case(M, N, K, act, bias, residual, seed=0, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    rows = 2 * N if act == SWIGLU else N
+    a, w = normal(g, (M, K), std).to(DEV), normal(g, (rows, K), 0.05).to(DEV)
+    b = normal(g, (rows,), 0.5).to(DEV) if bias else None
+    r = normal(g, (M, N), 2.0).to(DEV) if residual else None
+    return a, w, b, r
+
+
+def _want(a, w, b, r, act):
+    M, rows = a.shape[0], w.shape[0]
+    tap = torch.empty((M, rows), dtype=torch.float32, device=DEV)
+    lc.lacache_linear_bf16(a, w, torch.empty((M, rows), dtype=torch.bfloat16, device=DEV), tap)
+    x = tap.double() if b is None else tap.double() + b.double()
+    if act == SWIGLU:
+        N = rows // 2
+        y, t = _act(SWIGLU, x[:, :N])
+        u = x[:, N:]
+        t = t * u.abs() + y.abs() * u.abs() * 3 * U
+        y = y * u
+    else:
+        y, t = _act(act, x)
+    if r is not None:
+        y = y + r.double()
+        t = t + U * y.abs()
+    return y, t * (1 + 2.0 ** -7) + 2.0 ** -8 * y.abs() + 1e-38
+
+
+def _check(M, N, K, act, bias, residual, seed=0, std=1.0, in_place=False):
+    a, w, b, r = _case(M, N, K, act, bias, residual, seed, std)
+    want, tol = _want(a, w, b, r, act)
+    buf = torch.full((M * N + 256,), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = buf[128:128 + M * N].view(M, N)
+    if in_place:
+        out.copy_(r)
+        lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=out, act=act)
+    else:
+        lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=r, act=act)
+    torch.cuda.synchronize()
+    assert bool((buf[:128] == 7).all()) and bool((buf[128 + M * N:] == 7).all())
+    err = (out.double() - want).abs()
+    worst = float((err / tol).max())
+    print("M %d N %d K %d act %d: worst err/tolerance %.3f" % (M, N, K, act, worst), flush=True)
+    assert worst <= 1.0
+    return out
+
+
+# rows of every path: 1 to 4 slabs streamed, two passes, tiles of 128 and 256 rows, ragged ends
+ROWS = [1, 2, 16, 17, 32, 33, 48, 64, 65, 100, 128, 129, 200, 257, 1000]
+
+
+@pytest.mark.parametrize("act", range(6))
+@pytest.mark.parametrize("M", ROWS)
+def test_rows_and_activations(M, act):
+    _check(M, 384, 256, act, True, True, seed=M)
+
+
+@pytest.mark.parametrize("act", [GELU, SWIGLU])
+@pytest.mark.parametrize("bias,residual", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("M", [5, 70, 300])
+def test_optional_operands(M, bias, residual, act):
+    _check(M, 256, 128, act, bias, residual, seed=M + 1)
+
+
+@pytest.mark.parametrize("act", [NONE, SILU, SWIGLU])
+@pytest.mark.parametrize("M,N,K", [(1, 128, 128), (8, 12288, 256), (32, 12288, 512), (20, 128, 8192), (130, 128, 128),
+                                   (700, 1152, 640), (1500, 12288, 128), (2100, 3840, 192 * 2), (300, 640, 1024)])
+def test_sizes(M, N, K, act):
+    _check(M, N, K, act, True, True, seed=N + K)
+
+
+@pytest.mark.parametrize("M", [3, 40, 128, 129, 600])
+@pytest.mark.parametrize("act", [NONE, GELU_TANH, SWIGLU])
+def test_residual_updated_in_place(M, act):
+    x = _check(M, 256, 256, act, True, True, seed=M, in_place=True)
+    y = _check(M, 256, 256, act, True, True, seed=M)
+    assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+@pytest.mark.parametrize("M", [1, 64, 100, 300, 1500])
+def test_no_epilogue_is_the_plain_product_bit_for_bit(M):
+    a, w, _, _ = _case(M, 1152, 512, NONE, False, False, seed=M)
+    a[0, 3] = float("nan")
+    out, plain = (torch.empty((M, 1152), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lc.lacache_linear_act_bf16(a, w, out)
+    lc.lacache_linear_bf16(a, w, plain)
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), plain.view(torch.int16))
+
+
+@pytest.mark.parametrize("act", range(6))
+@pytest.mark.parametrize("M", [4, 200])
+def test_far_arguments_and_values_that_are_no_numbers(M, act):
+    """Sums of hundreds, where exp overflows; infinities and NaNs pass like the formula's."""
+    _check(M, 256, 256, act, True, False, seed=9, std=300.0)
+    a, w, b, r = _case(M, 128, 128, act, True, True, seed=10)
+    b[0], b[1], b[2] = float("inf"), float("-inf"), float("nan")
+    out = torch.empty((M, 128), dtype=torch.bfloat16, device=DEV)
+    lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=r, act=act)
+    torch.cuda.synchronize()
+    o = out.float()
+    assert bool((o[:, 0].abs() == math.inf).all()) and bool(torch.isfinite(o[:, 3:]).all())
+    assert bool(torch.isnan(o[:, 2]).all()) and bool((out[:, 2].view(torch.int16) == 0x7FC0).all())
+    if act == NONE:
+        assert bool((o[:, 1] == -math.inf).all())
+
+
+def test_captured_and_replayed():
+    a, w, b, r = _case(40, 256, 256, SILU, True, True, seed=11)
+    out = torch.empty((40, 256), dtype=torch.bfloat16, device=DEV)
+    lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=r, act=SILU)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=r, act=SILU)
+    for k in range(3):
+        a.mul_(-0.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        lc.lacache_linear_act_bf16(a, w, out, bias=b, residual=r, act=SILU)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), out.view(torch.int16)), k
