@@ -166,8 +166,12 @@ struct PagedAttn {
   int max_len;  // max_pages P
   int causal;
   float scale_log2;
+  // (set by the launcher)
+  float* part;    // the pieces' states
+  int row_tiles;  // of a KV head's rows
+  int wq;         // pieces aimed at per KV head and row tile
 };
-size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
-hipError_t launch_paged_attention(hipStream_t st, const PagedAttn& a, int64_t d, bool fp8, void* ws);
+size_t paged_attention_ws_bytes(int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
+hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws);
 
 }  // namespace lacache

@@ -76,69 +76,574 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
   }
 }
 
-// The value of an e4m3 code.
-__device__ __forceinline__ float e4m3_value(uint32_t code) {
-  return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(code), 0);
+// ---------------------------------------------------------------------------
+// Attention of the new tokens.
+//
+// The nq heads / kv_heads query rows of a KV head share its keys and values, so
+// they are the columns of one product: S^T = K Q^T, O^T = V^T P^T with 16x16x32
+// bf16 MFMAs, RT tiles of 16 rows. What a call cannot do without is one read of
+// the sequences' keys and values, and every choice serves that stream:
+//
+// A wavefront works alone on a run of key tiles (32 keys of 256 bytes, 64 of
+// fewer) through two LDS slots of its own, one of keys and one of values, each
+// refilled by direct copies as soon as it has been read: the next keys fly
+// during softmax and P V, the next values during the next scores, without a
+// barrier. Two workgroups of 4 wavefronts per CU keep 64 to 128 KB in flight.
+//
+// Work is cut on the device, where the lengths are: a sequence of nt tiles gets
+// n = ceil(nt Wq / sum nt) pieces (at most one per 4 tiles, one for an empty one),
+// Wq + S or fewer in all (below 2 Wq of them in sequences of more than one, since
+// n < 2 nt Wq / sum nt there), so that pieces are of about one length whatever the
+// batch; a piece's tiles are divided over the 4 wavefronts, whose states meet in
+// LDS. A sequence of one piece is finished there; those of others are joined by
+// paged_join_kernel, in piece order.
+//
+// Softmax in base 2 with the state (m, l, O) in fp32; P enters the second
+// product as two bf16 terms (p = hi + lo, 2^-17 relative: one term would double
+// the error of the rounded output, and the products are not what bounds the
+// call). e4m3 keys and values become bf16 exactly; a key's scale multiplies its
+// scores, a value's its P, both in fp32.
+//
+// Places that no row may see: keys behind the end or on no page get scores of
+// -inf and value rows of zeros in LDS (0 times a NaN would be one); in the tiles
+// where causal rows differ, values that are not finite send the tile through
+// one product per key, whose result the hiding rows do not take.
+// ---------------------------------------------------------------------------
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef int i2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef __attribute__((address_space(3))) i2 lds_i2;
+
+constexpr int kPagedWaves = 4;
+constexpr float kInf = __builtin_inff();
+
+// Sum over lanes 0 .. l of a wavefront.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of rows 0 and 2 to the rows above
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+  return x;
 }
 
-// Attention, plainly: a wavefront per query row; lane j takes key j of 64 for
-// the scores and dims j, j + 64 of the values.
-template <int D, bool kFp8>
-__global__ __launch_bounds__(64) void paged_attention_simple_kernel(PagedAttn a) {
-  __shared__ float sp[64];
-  __shared__ float sq[D];
-  const int lane = threadIdx.x;
-  const int h = blockIdx.x % a.heads, t = (blockIdx.x / a.heads) % a.nq;
-  const int64_t s = blockIdx.x / (a.heads * a.nq), row = blockIdx.x;
-  const int kvh = h / (a.heads / a.kv_heads);
-  int len = a.seq_lens[s];
-  len = len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
-  const int end = a.causal ? len - a.nq + t + 1 : len;
-  for (int i = lane; i < D; i += 64) sq[i] = bf16lo(a.q[row * D + i]);
-  __syncthreads();
-  float m = -__builtin_inff(), l = 0.0f, o[D / 64] = {};
-  for (int k0 = 0; k0 < end; k0 += 64) {
-    const int key = k0 + lane;
-    float x = -__builtin_inff();
-    int64_t kr = -1;
-    if (key < end) {
-      const int page = a.table[s * a.max_pages + (key >> a.page_log2)];
-      if (page >= 0 && page < a.num_pages) {
-        kr = ((static_cast<int64_t>(page) * a.kv_heads + kvh) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
-        float dot = 0.0f;
-        for (int i = 0; i < D; ++i) {
-          const float kvv = kFp8 ? e4m3_value(static_cast<const uint8_t*>(a.k_cache)[kr * D + i])
-                                 : bf16lo(static_cast<const uint16_t*>(a.k_cache)[kr * D + i]);
-          dot += sq[i] * kvv;
-        }
-        if (kFp8) dot *= a.k_scale[kr];
-        x = dot * a.scale_log2;
-      }
+__device__ __forceinline__ int seq_len(const PagedAttn& a, int s) {
+  const int len = a.seq_lens[s];
+  return len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
+}
+
+// Key tiles of all sequences (every lane).
+template <int kKeys>
+__device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
+  int n = 0;
+  for (int b = 0; b < a.S; b += 64)
+    if (b + lane < a.S) n += (seq_len(a, b + lane) + kKeys - 1) / kKeys;
+  return __builtin_amdgcn_readlane(wave_prefix(n), 63);
+}
+
+// Pieces of a sequence of nt tiles.
+__device__ __forceinline__ int pieces(int nt, int tot, int wq) {
+  const int n = nt == 0 ? 1 : static_cast<int>((static_cast<uint32_t>(nt) * static_cast<uint32_t>(wq) + tot - 1) / tot);
+  const int most = (nt + kPagedWaves - 1) / kPagedWaves;
+  return n < most ? n : (most < 1 ? 1 : most);
+}
+
+template <int D, bool kFp8, int RT>
+struct PagedTile {
+  static constexpr int RB = D * (kFp8 ? 1 : 2);       // bytes of a key
+  // keys of a tile (32 also where 64 would not fit the registers)
+  static constexpr int kKeys = RB == 256 || (D == 128 && RT == 2) ? 32 : 64;
+  static constexpr int kBytes = kKeys * RB;           // of an LDS slot
+  static constexpr int CPR = RB / 16;                 // 16-byte chunks of a key
+  static constexpr int KPI = 1024 / RB;               // keys of a copy instruction
+  static constexpr int UPS = 16 / KPI;                // copies of 16 keys
+  static constexpr int kSub = kKeys / 16;
+  static constexpr int kCopies = kBytes / 1024 + (kFp8 ? 1 : 0);  // of keys or values, with their scales
+  static constexpr int kSlot = 2 * kBytes + (kFp8 ? 2 * 64 * 4 : 0);  // a wavefront's LDS
+};
+// A key's 16-byte chunk c lies at c ^ swizzle: keys are read 16 at a time, one
+// chunk of each, values (transposed) in 8 or 16 keys by 32 or 16 bytes, and both
+// then touch every bank once. kU: the part that a copy adds, by its number.
+template <int RB>
+__device__ __forceinline__ int kswz(int key) {
+  return RB == 256 ? key & 15 : (RB == 128 ? (key >> 1) & 7 : (key >> 2) & 3);
+}
+template <int RB, bool kFp8>
+__device__ __forceinline__ int vswz(int key) {
+  if (RB == 256) return 2 * (key & 7);
+  if (RB == 128 && !kFp8) return 2 * ((key >> 1) & 3);
+  if (RB == 128) return ((key >> 1) & 3) | ((key >> 2) & 4);
+  return ((key >> 2) & 1) | ((key >> 3) & 2);
+}
+
+__device__ __forceinline__ bf8 cvt_fp8x8(uint32_t lo, uint32_t hi) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  const b2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const b2 x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const b2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const b2 x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return bf8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+}
+
+__device__ __forceinline__ v4f mfma16(bf8 a, bf8 b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float finite_max(float m) { return m == -kInf ? 0.0f : m; }
+
+// The output row (an index of [S x nq x heads]) of row rr of KV head h.
+__device__ __forceinline__ int64_t out_row(const PagedAttn& a, int s, int h, int rr) {
+  const int G = a.heads / a.kv_heads, t = rr / G;
+  return (static_cast<int64_t>(s) * a.nq + t) * a.heads + h * G + (rr - t * G);
+}
+
+__device__ __forceinline__ void store_out(const PagedAttn& a, int64_t row, int D, int c4, v4f o, float m, float l) {
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  *reinterpret_cast<uint2*>(a.o + row * D + 4 * c4) =
+      make_uint2(cvt_pk_bf16(o[0] * inv, o[1] * inv), cvt_pk_bf16(o[2] * inv, o[3] * inv));
+  if (a.lse != nullptr && c4 == 0) a.lse[row] = (m + __log2f(l)) * 0.69314718055994531f;
+}
+
+template <int D, bool kFp8, int RT>
+__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(PagedAttn a) {
+  using T = PagedTile<D, kFp8, RT>;
+  constexpr int RB = T::RB, kKeys = T::kKeys, kSub = T::kSub, kRows = 16 * RT, kSteps = D / 32, kDims = D / 16;
+  constexpr int kState = kRows * D * 4;  // a wavefront's O at the end
+  constexpr int kSlot = T::kSlot > kState ? T::kSlot : kState;
+  __shared__ __align__(16) uint8_t smem[kPagedWaves * kSlot];
+  __shared__ float sml[2][kPagedWaves][kRows];
+  const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
+  const int g = lane >> 4, r = lane & 15;
+
+  // the work item: row tiles of one (piece, KV head) together on an XCD
+  const int rt_n = a.row_tiles, per = 8 * rt_n;
+  const int q8 = blockIdx.x / per, rem = blockIdx.x - q8 * per;
+  const int rt = rem >> 3, pair = q8 * 8 + (rem & 7);
+  const int h = pair % a.kv_heads;
+  int unit = pair / a.kv_heads;
+  const int tot = total_tiles<kKeys>(a, lane);
+  int s = -1, n = 0, slot = 0;  // slot: the place of the sequence's first piece in the workspace
+  for (int b = 0; b < a.S; b += 64) {
+    const int mine = b + lane < a.S ? pieces((seq_len(a, b + lane) + kKeys - 1) / kKeys, tot, a.wq) : 0;
+    const int upto = wave_prefix(mine), kept = wave_prefix(mine > 1 ? mine : 0);
+    const uint64_t behind = __ballot(upto > unit);
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind);
+      s = b + at;
+      n = __builtin_amdgcn_readlane(mine, at);
+      unit -= __builtin_amdgcn_readlane(upto, at) - n;
+      slot += __builtin_amdgcn_readlane(kept, at) - n;
+      break;
     }
-    const float mn = __builtin_fmaxf(m, max_xor<64>(x));
-    const float ms = mn == -__builtin_inff() ? 0.0f : mn;
-    const float alpha = __builtin_amdgcn_exp2f(m - ms), p = __builtin_amdgcn_exp2f(x - ms);
-    m = mn;
-    l = l * alpha + p;
-    for (int e = 0; e < D / 64; ++e) o[e] *= alpha;
-    __syncthreads();
-    sp[lane] = kFp8 && kr >= 0 ? p * a.v_scale[kr] : p;
-    __syncthreads();
-    for (int j = 0; j < 64; ++j) {
-      const int64_t r = __shfl(kr, j, 64);
-      if (r < 0) continue;
-      for (int e = 0; e < D / 64; ++e) {
-        const int64_t i = r * D + 64 * e + lane;
-        const float vv = kFp8 ? e4m3_value(static_cast<const uint8_t*>(a.v_cache)[i])
-                              : bf16lo(static_cast<const uint16_t*>(a.v_cache)[i]);
-        o[e] += sp[j] * vv;
-      }
+    unit -= __builtin_amdgcn_readlane(upto, 63);
+    slot += __builtin_amdgcn_readlane(kept, 63);
+  }
+  if (s < 0) return;  // (fewer pieces than the grid has room for)
+  const int len = wave_uniform(seq_len(a, s));
+  const int nt = (len + kKeys - 1) / kKeys;
+  // (below 2^32: unit < n <= 4 compute units, nt <= 2^17)
+  const int p0 = static_cast<int>(static_cast<uint32_t>(unit) * static_cast<uint32_t>(nt) / n);
+  const int p1 = static_cast<int>(static_cast<uint32_t>(unit + 1) * static_cast<uint32_t>(nt) / n);
+  const int i0 = p0 + wave * (p1 - p0) / kPagedWaves, i1 = p0 + (wave + 1) * (p1 - p0) / kPagedWaves;
+
+  // Q^T operands: row kRows rt + 16 x + r, the dims that the K operand's lanes read together
+  const int G = a.heads / a.kv_heads, R = a.nq * G;
+  bf8 qf[RT][kSteps];
+  int limit[RT];  // keys that this lane's row sees
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    const int rr = kRows * rt + 16 * x + r;
+    limit[x] = a.causal ? len - a.nq + rr / G + 1 : len;
+    const uint16_t* src = a.q + out_row(a, s, h, rr < R ? rr : 0) * D;
+#pragma unroll
+    for (int ks = 0; ks < kSteps; ++ks) {
+      const int dim = kFp8 ? 64 * (ks >> 1) + 16 * g + 8 * (ks & 1) : 32 * ks + 8 * g;
+      qf[x][ks] = *reinterpret_cast<const bf8*>(src + dim);
     }
   }
-  for (int x = 32; x >= 1; x >>= 1) l += __shfl_xor(l, x, 64);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  for (int e = 0; e < D / 64; ++e) a.o[row * D + 64 * e + lane] = static_cast<uint16_t>(f32_to_bf16(o[e] * inv));
-  if (a.lse != nullptr && lane == 0) a.lse[row] = (m + __log2f(l)) * 0.69314718055994531f;
+  const int shared_end = a.causal ? len - a.nq + 1 : len;  // keys that every row sees
+
+  float m[RT], l[RT];
+  v4f ot[RT][kDims];
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    m[x] = -kInf, l[x] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) ot[x][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  uint8_t* const Kt = smem + wave * kSlot;
+  uint8_t* const Vt = Kt + T::kBytes;
+  const float* const Ks = reinterpret_cast<const float*>(Vt + T::kBytes);
+  const float* const Vs = Ks + 64;
+  const uint32_t lds = lds_u32(Kt);
+
+  // pages: lane x holds that of keys 16 (sb + x) ..; -1: not to be read
+  int sb = 0, pages = -1;
+  const int32_t* table = a.table + static_cast<int64_t>(s) * a.max_pages;
+  auto load_pages = [&](int first) {
+    sb = first;
+    const int key = (first + lane) * 16;
+    const int page = table[(key < a.max_len ? key : a.max_len - 1) >> a.page_log2];
+    pages = key < len && page < static_cast<int>(a.num_pages) ? page : -1;
+    // (known to the compiler, which would else wait for every copy at each use)
+    wait_vm<0>();
+  };
+  // the row of the caches of keys 16 (sb + x) .., or -1
+  auto row_of = [&](int sub) -> int64_t {
+    const int page = __builtin_amdgcn_readlane(pages, sub - sb);
+    const int in = (sub * 16) & ((1 << a.page_log2) - 1);
+    const int64_t row = page < 0 ? -1 : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
+    // (the same in every lane, and the copies take it from scalar registers)
+    return static_cast<int64_t>(static_cast<uint32_t>(wave_uniform(static_cast<int>(row)))) |
+           (static_cast<int64_t>(wave_uniform(static_cast<int>(row >> 32))) << 32);
+  };
+  const int ckey = lane / T::CPR, cch = lane % T::CPR;
+  const uint32_t koff = ckey * RB + ((cch ^ kswz<RB>(ckey)) << 4);
+  const uint32_t voff = ckey * RB + ((cch ^ vswz<RB, kFp8>(ckey)) << 4);
+  // (fresh: keeps the compiler from holding what is derived from it in registers across the loop)
+  auto fresh = [](auto v) {
+    asm volatile("" : "+v"(v));
+    return v;
+  };
+  auto issue = [&](int i, bool values) {
+    const uint32_t off = fresh(values ? voff : koff);
+    const uint8_t* cache = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache);
+    const uint32_t dst = lds + (values ? T::kBytes : 0);
+#pragma unroll
+    for (int tt = 0; tt < kSub; ++tt) {
+      const int64_t row = row_of(i * kSub + tt);
+      // (16 keys of no page: any that exist; they are not used)
+      const uint8_t* src = cache + (row < 0 ? 0 : row) * RB;
+#pragma unroll
+      for (int u = 0; u < T::UPS; ++u) {
+        const int first = 16 * tt + T::KPI * u;
+        const uint32_t x = static_cast<uint32_t>(values ? vswz<RB, kFp8>(first) : kswz<RB>(first)) << 4;
+        dma16s(src + u * 1024, off ^ x, wave_uniform(static_cast<int>(dst + (tt * T::UPS + u) * 1024)));
+      }
+    }
+    if (kFp8) {
+      // a scale per lane (of a tile of 32 keys twice)
+      const int page = __shfl(pages, i * kSub - sb + (g & (kSub - 1)), 64);
+      const int in = (i * kKeys + (lane & (kKeys - 1))) & ((1 << a.page_log2) - 1);
+      const int64_t row = page < 0 ? r : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
+      dma4((values ? a.v_scale : a.k_scale) + row,
+           wave_uniform(static_cast<int>(lds + 2 * T::kBytes + (values ? 256 : 0))));
+    }
+  };
+
+  // per-lane LDS offsets: K operand chunk 4 step + g of key r; V^T operand (transposing
+  // reads) of keys 4 g .. + 3 and 16 + 4 g .. + 3, dims 16 d ..
+  const int k_base = r * RB + ((g ^ kswz<RB>(r)) << 4);
+  const int vkey = kFp8 ? ((r >> 1) < 4 ? 4 * g + (r >> 1) : 12 + 4 * g + (r >> 1)) : 4 * g + (r >> 2);
+  const int v_base = vkey * RB + (vswz<RB, kFp8>(vkey) << 4) +
+                     (kFp8 ? 8 * (r & 1) : ((((r & 3) >> 1) << 4) | (8 * (r & 1))));
+  auto value_operand = [&](int v_base, int step, int d) -> bf8 {
+    if constexpr (kFp8) {
+      const i2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(Vt + 32 * step * RB + (v_base ^ (d << 4))));
+      return cvt_fp8x8(static_cast<uint32_t>(w[0]), static_cast<uint32_t>(w[1]));
+    } else {
+      const uint8_t* p = Vt + 32 * step * RB + (v_base ^ (d << 5));
+      const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p));
+      const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 16 * RB));
+      return __builtin_bit_cast(bf8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
+
+  load_pages(i0 * kSub);
+  if (i0 < i1) {
+    issue(i0, false);
+    issue(i0, true);
+  }
+  for (int i = i0; i < i1; ++i) {
+    const bool more = i + 1 < i1;
+    // keys of the tile that exist: a prefix of each 16
+    int cnt[kSub];
+    bool whole = true;
+#pragma unroll
+    for (int tt = 0; tt < kSub; ++tt) {
+      const int left = len - (i * kKeys + 16 * tt);
+      cnt[tt] = __builtin_amdgcn_readlane(pages, i * kSub + tt - sb) < 0 ? 0 : (left > 16 ? 16 : (left < 0 ? 0 : left));
+      whole &= cnt[tt] == 16;
+    }
+    const bool differ = (i + 1) * kKeys > shared_end;  // some row does not see all of them
+
+    wait_vm<T::kCopies>();  // the keys have landed
+    const int kb = fresh(k_base);
+    v4f sc[RT][kSub];
+#pragma unroll
+    for (int tt = 0; tt < kSub; ++tt) {
+#pragma unroll
+      for (int x = 0; x < RT; ++x) sc[x][tt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      if constexpr (kFp8) {
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ks += 2) {
+          const uint4 w = *reinterpret_cast<const uint4*>(Kt + 16 * tt * RB + (kb ^ (ks << 5)));
+          const bf8 k0 = cvt_fp8x8(w.x, w.y), k1 = cvt_fp8x8(w.z, w.w);
+#pragma unroll
+          for (int x = 0; x < RT; ++x) sc[x][tt] = mfma16(k1, qf[x][ks + 1], mfma16(k0, qf[x][ks], sc[x][tt]));
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) {
+          const bf8 kf = *reinterpret_cast<const bf8*>(Kt + 16 * tt * RB + (kb ^ (ks << 6)));
+#pragma unroll
+          for (int x = 0; x < RT; ++x) sc[x][tt] = mfma16(kf, qf[x][ks], sc[x][tt]);
+        }
+      }
+    }
+    v4f kscale[kSub];
+    if (kFp8) {
+#pragma unroll
+      for (int tt = 0; tt < kSub; ++tt) kscale[tt] = *reinterpret_cast<const v4f*>(Ks + 16 * tt + 4 * g) * a.scale_log2;
+    }
+    wait_lds();
+    if (more) {
+      if ((i + 1) * kSub - sb >= 64) load_pages((i + 1) * kSub);
+      issue(i + 1, false);
+    }
+
+    // scores in base 2; hidden ones -inf
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+      for (int tt = 0; tt < kSub; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[x][tt][e] *= kFp8 ? kscale[tt][e] : a.scale_log2;
+    if (!whole || differ) {
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int tt = 0; tt < kSub; ++tt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * g + e >= cnt[tt] || i * kKeys + 16 * tt + 4 * g + e >= limit[x]) sc[x][tt][e] = -kInf;
+    }
+    bf8 ph[RT][kKeys / 32], pl[RT][kKeys / 32];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      float mx = sc[x][0][0];
+#pragma unroll
+      for (int tt = 0; tt < kSub; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = __builtin_fmaxf(mx, sc[x][tt][e]);
+      mx = __builtin_fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = __builtin_fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = __builtin_fmaxf(m[x], mx), ms = finite_max(mn);
+      const float alpha = __builtin_amdgcn_exp2f(m[x] - ms);
+      m[x] = mn;
+      float sum = 0.0f;
+#pragma unroll
+      for (int tt = 0; tt < kSub; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(sc[x][tt][e] - ms);
+          sc[x][tt][e] = p;
+          sum += p;
+        }
+      l[x] = l[x] * alpha + sum;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ot[x][d][e] *= alpha;
+    }
+
+    if (more)
+      wait_vm<T::kCopies>();  // the values have landed (the next keys may be in flight)
+    else
+      wait_vm<0>();
+    if (kFp8) {
+#pragma unroll
+      for (int tt = 0; tt < kSub; ++tt) {
+        const v4f vs = *reinterpret_cast<const v4f*>(Vs + 16 * tt + 4 * g);
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = sc[x][tt][e] * vs[e];
+            // (a hidden key's scale may be no number)
+            const bool hide = (!whole || differ) &&
+                              (4 * g + e >= cnt[tt] || i * kKeys + 16 * tt + 4 * g + e >= limit[x]);
+            sc[x][tt][e] = hide ? 0.0f : p;
+          }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+      for (int st = 0; st < kKeys / 32; ++st) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const v4f& p = sc[x][2 * st + (e >> 1)];
+          const float p0 = p[2 * (e & 1)], p1 = p[2 * (e & 1) + 1];
+          hi[e] = cvt_pk_bf16(p0, p1);
+          lo[e] = cvt_pk_bf16(p0 - bf16lo(hi[e]), p1 - bf16hi(hi[e]));
+        }
+        ph[x][st] = __builtin_bit_cast(bf8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        pl[x][st] = __builtin_bit_cast(bf8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      }
+    if (!whole) {
+      // values of keys that do not exist: zeros
+      uint8_t* const mine = Vt + fresh(lane * 16);
+#pragma unroll
+      for (int u = 0; u < T::kBytes / 1024; ++u) {
+        const int key = T::KPI * u + ckey;  // (one 16 of the tile per copy)
+        if ((key & 15) >= cnt[(T::KPI * u) >> 4]) *reinterpret_cast<uint4*>(mine + u * 1024) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      asm volatile("" ::: "memory");
+    }
+    bool odd = false;
+    if (a.causal && differ) {
+      // is every value finite?
+      uint32_t bad = 0u;
+      const uint8_t* const mine = Vt + fresh(lane * 16);
+#pragma unroll 1
+      for (int u = 0; u < T::kBytes / 1024; ++u) {
+        const uint4 w4 = *reinterpret_cast<const uint4*>(mine + u * 1024);
+        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          bad |= kFp8 ? (((w[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)
+                      : (((w[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u);
+      }
+      odd = __any(bad != 0u);
+    }
+    const int vb = fresh(v_base);
+    if (!odd) {
+#pragma unroll
+      for (int st = 0; st < kKeys / 32; ++st)
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+          const bf8 vf = value_operand(vb, st, d);
+#pragma unroll
+          for (int x = 0; x < RT; ++x) ot[x][d] = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
+        }
+    } else {
+#pragma unroll
+      for (int st = 0; st < kKeys / 32; ++st)
+#pragma unroll 1
+        for (int kk = 0; kk < 32; ++kk) {
+          // key kk of the step: element 4 (kk / 16) + kk % 4 of the lanes of group (kk / 4) % 4
+          const int el = 4 * (kk >> 4) + (kk & 3), key = i * kKeys + 32 * st + kk;
+          const bool mine = g == ((kk >> 2) & 3);
+#pragma unroll
+          for (int d = 0; d < kDims; ++d) {
+            uint4 w = __builtin_bit_cast(uint4, value_operand(vb, st, d));
+            uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ww[e] = mine && (el >> 1) == e ? (el & 1 ? ww[e] & 0xFFFF0000u : ww[e] & 0xFFFFu) : 0u;
+            const bf8 vf = __builtin_bit_cast(bf8, make_uint4(ww[0], ww[1], ww[2], ww[3]));
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+              const v4f sum = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) ot[x][d][e] = key < limit[x] ? sum[e] : ot[x][d][e];
+            }
+          }
+        }
+    }
+    wait_lds();
+    if (more) issue(i + 1, true);
+  }
+
+  // the wavefronts' states meet: O of row x at 16-byte chunk c ^ row
+#pragma unroll
+  for (int x = 0; x < RT; ++x) {
+    l[x] += __shfl_xor(l[x], 16, 64);
+    l[x] += __shfl_xor(l[x], 32, 64);
+    if (g == 0) sml[0][wave][16 * x + r] = m[x], sml[1][wave][16 * x + r] = l[x];
+#pragma unroll
+    for (int d = 0; d < kDims; ++d)
+      *reinterpret_cast<v4f*>(Kt + (16 * x + r) * D * 4 + (((4 * d + g) ^ r) << 4)) = ot[x][d];
+  }
+  __syncthreads();
+  constexpr int C4 = D / 4;
+  float* part = a.part + (static_cast<int64_t>(slot + unit) * a.kv_heads * rt_n + h * rt_n + rt) * (kRows * (D + 2));
+#pragma unroll
+  for (int e = t; e < kRows * C4; e += 64 * kPagedWaves) {
+    const int row = e / C4, c4 = e - row * C4, rr = kRows * rt + row;
+    if (rr >= R) continue;
+    float mm = -kInf;
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) mm = __builtin_fmaxf(mm, sml[0][w][row]);
+    const float ms = finite_max(mm);
+    float ll = 0.0f;
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sml[0][w][row] - ms);
+      ll += f * sml[1][w][row];
+      const v4f x = *reinterpret_cast<const v4f*>(smem + w * kSlot + row * D * 4 + ((c4 ^ (row & 15)) << 4));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += f * x[k];
+    }
+    if (n == 1) {
+      store_out(a, out_row(a, s, h, rr), D, c4, o, mm, ll);
+    } else {
+      *reinterpret_cast<v4f*>(part + 2 * kRows + row * D + 4 * c4) = o;
+      if (c4 == 0) part[row] = mm, part[kRows + row] = ll;
+    }
+  }
+}
+
+// Joins the pieces of (sequence, KV head, row tile) blockIdx.x: thread (row, 4
+// dims) adds its pieces in order.
+template <int D, int kKeys, int RT>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
+  constexpr int kRows = 16 * RT, C4 = D / 4, kPart = kRows * (D + 2);
+  const int t = threadIdx.x, lane = t & 63;
+  const int hr = blockIdx.x % (a.kv_heads * a.row_tiles), s = blockIdx.x / (a.kv_heads * a.row_tiles);
+  const int tot = total_tiles<kKeys>(a, lane);
+  const int n = pieces((seq_len(a, s) + kKeys - 1) / kKeys, tot, a.wq);
+  if (n == 1) return;
+  int before = 0;
+  for (int b = 0; b < s; b += 64)
+    if (b + lane < s) {
+      const int k = pieces((seq_len(a, b + lane) + kKeys - 1) / kKeys, tot, a.wq);
+      before += k > 1 ? k : 0;
+    }
+  before = __builtin_amdgcn_readlane(wave_prefix(before), 63);
+  const int h = hr / a.row_tiles, rt = hr - h * a.row_tiles;
+  const int R = a.nq * (a.heads / a.kv_heads);
+  const int64_t stride = static_cast<int64_t>(a.kv_heads) * a.row_tiles * kPart;
+  const float* part = a.part + before * stride + static_cast<int64_t>(hr) * kPart;
+  for (int e = t; e < kRows * C4; e += 256) {
+    const int row = e / C4, c4 = e - row * C4, rr = kRows * rt + row;
+    if (rr >= R) break;
+    float mm = -kInf;
+    for (int p = 0; p < n; ++p) mm = __builtin_fmaxf(mm, part[p * stride + row]);
+    const float ms = finite_max(mm);
+    float ll = 0.0f;
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float* x = part + p * stride;
+      const float f = __builtin_amdgcn_exp2f(x[row] - ms);
+      ll += f * x[kRows + row];
+      const v4f y = *reinterpret_cast<const v4f*>(x + 2 * kRows + row * D + 4 * c4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += f * y[k];
+    }
+    store_out(a, out_row(a, s, h, rr), D, c4, o, mm, ll);
+  }
+}
+
+// Row tiles of 16 for up to 16 rows per KV head, else of 32.
+int paged_rt(int64_t R) { return R <= 16 ? 1 : 2; }
+struct PagedPlan {
+  int64_t row_tiles, wq, parts;  // parts: piece states that a call may keep
+};
+PagedPlan paged_plan(int64_t nq, int64_t heads, int64_t kv_heads) {
+  const int64_t R = nq * (heads / kv_heads), rows = 16 * paged_rt(R);
+  PagedPlan p;
+  p.row_tiles = (R + rows - 1) / rows;
+  const int64_t hr = kv_heads * p.row_tiles;
+  p.wq = (4 * device_cu_count() + hr - 1) / hr;
+  p.parts = p.wq == 1 ? 0 : 2 * p.wq * hr;
+  return p;
 }
 
 }  // namespace
@@ -158,18 +663,38 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
   return hipGetLastError();
 }
 
-size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
-  (void)S, (void)nq, (void)heads, (void)kv_heads, (void)d;
-  return 256;
+size_t paged_attention_ws_bytes(int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
+  const PagedPlan p = paged_plan(nq, heads, kv_heads);
+  const size_t bytes = 256 + static_cast<size_t>(p.parts) * 16 * paged_rt(nq * (heads / kv_heads)) * (d + 2) * 4;
+  return (bytes + 255) / 256 * 256;
 }
 
-hipError_t launch_paged_attention(hipStream_t st, const PagedAttn& a, int64_t d, bool fp8, void* ws) {
-  (void)ws;
-  const dim3 grid(static_cast<unsigned>(a.S) * a.nq * a.heads), block(64);
-  if (d == 128 && fp8) hipLaunchKernelGGL((paged_attention_simple_kernel<128, true>), grid, block, 0, st, a);
-  else if (d == 128) hipLaunchKernelGGL((paged_attention_simple_kernel<128, false>), grid, block, 0, st, a);
-  else if (fp8) hipLaunchKernelGGL((paged_attention_simple_kernel<64, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((paged_attention_simple_kernel<64, false>), grid, block, 0, st, a);
+hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws) {
+  const PagedPlan p = paged_plan(a.nq, a.heads, a.kv_heads);
+  a.part = static_cast<float*>(ws);
+  a.row_tiles = static_cast<int>(p.row_tiles);
+  a.wq = static_cast<int>(p.wq);
+  const int64_t pairs = (p.wq + a.S) * a.kv_heads;
+  const dim3 grid(static_cast<unsigned>((pairs + 7) / 8 * 8 * p.row_tiles)), block(64 * kPagedWaves);
+  const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles));
+  // (no sequence of several pieces: nothing to join)
+  const bool join = p.wq > 1 && a.max_len > kPagedWaves * 32;
+#define PA(D_, F_, RT_)                                                                                      \
+  do {                                                                                                       \
+    hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                        \
+    if (join) hipLaunchKernelGGL((paged_join_kernel<D_, PagedTile<D_, F_, RT_>::kKeys, RT_>), jgrid, dim3(256), 0, st, a);  \
+  } while (0)
+#define PR(D_, F_)                                                 \
+  do {                                                             \
+    if (paged_rt(static_cast<int64_t>(a.nq) * (a.heads / a.kv_heads)) == 1) PA(D_, F_, 1); \
+    else PA(D_, F_, 2);                                            \
+  } while (0)
+  if (d == 128 && fp8) PR(128, true);
+  else if (d == 128) PR(128, false);
+  else if (fp8) PR(64, true);
+  else PR(64, false);
+#undef PR
+#undef PA
   return hipGetLastError();
 }
 
