@@ -143,11 +143,13 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
   return __builtin_amdgcn_readlane(wave_prefix(n), 63);
 }
 
-// Pieces of a sequence of nt tiles.
+// Pieces of a sequence of nt tiles. One of at most kWhole tiles stays whole: four
+// tiles one after the other in each wavefront cost less than a second kernel.
+constexpr int kWhole = 4 * kPagedWaves;
 __device__ __forceinline__ int pieces(int nt, int tot, int wq) {
-  const int n = nt == 0 ? 1 : static_cast<int>((static_cast<uint32_t>(nt) * static_cast<uint32_t>(wq) + tot - 1) / tot);
+  const int n = nt <= kWhole ? 1 : static_cast<int>((static_cast<uint32_t>(nt) * static_cast<uint32_t>(wq) + tot - 1) / tot);
   const int most = (nt + kPagedWaves - 1) / kPagedWaves;
-  return n < most ? n : (most < 1 ? 1 : most);
+  return n < most || n == 1 ? n : most;
 }
 
 template <int D, bool kFp8, int RT>
@@ -589,13 +591,19 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   }
 }
 
-// Joins the pieces of (sequence, KV head, row tile) blockIdx.x: thread (row, 4
-// dims) adds its pieces in order.
+// Joins the pieces of a (sequence, KV head, row tile), 32 dims of them per
+// workgroup: 8 threads per (row, share of the pieces), the shares (every pg-th
+// piece, in order) joined through LDS in order. Each thread has kAhead pieces'
+// loads in flight, and a long sequence's pieces are spread over up to 32 shares:
+// one thread per 4 dims walking 128 pieces took 95 us (one row of 131072 keys).
 template <int D, int kKeys, int RT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
-  constexpr int kRows = 16 * RT, C4 = D / 4, kPart = kRows * (D + 2);
+  constexpr int kRows = 16 * RT, kPart = kRows * (D + 2), kAhead = 4;
+  __shared__ __align__(16) float so[32][8][4];
+  __shared__ float sm[32], sl[32];
   const int t = threadIdx.x, lane = t & 63;
-  const int hr = blockIdx.x % (a.kv_heads * a.row_tiles), s = blockIdx.x / (a.kv_heads * a.row_tiles);
+  const int hrs = a.kv_heads * a.row_tiles;
+  const int hr = blockIdx.x % hrs, s = blockIdx.x / hrs;
   const int tot = total_tiles<kKeys>(a, lane);
   const int n = pieces((seq_len(a, s) + kKeys - 1) / kKeys, tot, a.wq);
   if (n == 1) return;
@@ -607,28 +615,62 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
     }
   before = __builtin_amdgcn_readlane(wave_prefix(before), 63);
   const int h = hr / a.row_tiles, rt = hr - h * a.row_tiles;
-  const int R = a.nq * (a.heads / a.kv_heads);
-  const int64_t stride = static_cast<int64_t>(a.kv_heads) * a.row_tiles * kPart;
+  const int left = a.nq * (a.heads / a.kv_heads) - kRows * rt, rows = left < kRows ? left : kRows;
+  const int rows2 = rows <= 1 ? 1 : 1 << (32 - __builtin_clz(rows - 1)), pg = 32 / rows2;
+  const int64_t stride = static_cast<int64_t>(hrs) * kPart;
   const float* part = a.part + before * stride + static_cast<int64_t>(hr) * kPart;
-  for (int e = t; e < kRows * C4; e += 256) {
-    const int row = e / C4, c4 = e - row * C4, rr = kRows * rt + row;
-    if (rr >= R) break;
-    float mm = -kInf;
-    for (int p = 0; p < n; ++p) mm = __builtin_fmaxf(mm, part[p * stride + row]);
-    const float ms = finite_max(mm);
-    float ll = 0.0f;
-    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const float* x = part + p * stride;
-      const float f = __builtin_amdgcn_exp2f(x[row] - ms);
-      ll += f * x[kRows + row];
-      const v4f y = *reinterpret_cast<const v4f*>(x + 2 * kRows + row * D + 4 * c4);
+  const int c = t & 7, u = t >> 3, row = u & (rows2 - 1), share = u / rows2, c4 = 8 * blockIdx.y + c;
+  float m = -kInf, l = 0.0f;
+  v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (row < rows) {
+    for (int p = share; p < n; p += kAhead * pg) {
+      float pm[kAhead], pl[kAhead];
+      v4f po[kAhead];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += f * y[k];
+      for (int k = 0; k < kAhead; ++k) {
+        const int q = p + k * pg;
+        const float* x = part + (q < n ? q : p) * stride;
+        pm[k] = q < n ? x[row] : -kInf;
+        pl[k] = x[kRows + row];
+        po[k] = *reinterpret_cast<const v4f*>(x + 2 * kRows + row * D + 4 * c4);
+      }
+      float mn = m;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) mn = __builtin_fmaxf(mn, pm[k]);
+      const float ms = finite_max(mn), f = __builtin_amdgcn_exp2f(m - ms);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (p + k * pg >= n) break;
+        const float fk = __builtin_amdgcn_exp2f(pm[k] - ms);
+        l += fk * pl[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += fk * po[k][e];
+      }
     }
-    store_out(a, out_row(a, s, h, rr), D, c4, o, mm, ll);
   }
+  *reinterpret_cast<v4f*>(so[u][c]) = o;
+  if (c == 0) sm[u] = m, sl[u] = l;
+  __syncthreads();
+  if (share != 0 || row >= rows) return;
+  float mm = m;
+  for (int k = 1; k < pg; ++k) mm = __builtin_fmaxf(mm, sm[row + k * rows2]);
+  const float ms = finite_max(mm), f = __builtin_amdgcn_exp2f(m - ms);
+  l *= f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= f;
+  for (int k = 1; k < pg; ++k) {
+    const int w = row + k * rows2;
+    const float fk = __builtin_amdgcn_exp2f(sm[w] - ms);
+    l += fk * sl[w];
+    const v4f x = *reinterpret_cast<const v4f*>(so[w][c]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += fk * x[e];
+  }
+  store_out(a, out_row(a, s, h, kRows * rt + row), D, c4, o, mm, l);
 }
 
 // Row tiles of 16 for up to 16 rows per KV head, else of 32.
@@ -676,13 +718,14 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   a.wq = static_cast<int>(p.wq);
   const int64_t pairs = (p.wq + a.S) * a.kv_heads;
   const dim3 grid(static_cast<unsigned>((pairs + 7) / 8 * 8 * p.row_tiles)), block(64 * kPagedWaves);
-  const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles));
+  const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles), static_cast<unsigned>(d / 32));
   // (no sequence of several pieces: nothing to join)
-  const bool join = p.wq > 1 && a.max_len > kPagedWaves * 32;
-#define PA(D_, F_, RT_)                                                                                      \
-  do {                                                                                                       \
-    hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                        \
-    if (join) hipLaunchKernelGGL((paged_join_kernel<D_, PagedTile<D_, F_, RT_>::kKeys, RT_>), jgrid, dim3(256), 0, st, a);  \
+#define PA(D_, F_, RT_)                                                                                     \
+  do {                                                                                                      \
+    constexpr int keys = PagedTile<D_, F_, RT_>::kKeys;                                                     \
+    hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                       \
+    if (p.wq > 1 && a.max_len > kWhole * keys)                                                              \
+      hipLaunchKernelGGL((paged_join_kernel<D_, keys, RT_>), jgrid, dim3(256), 0, st, a);                   \
   } while (0)
 #define PR(D_, F_)                                                 \
   do {                                                             \
