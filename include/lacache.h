@@ -435,8 +435,9 @@ size_t lacache_first_layer_workspace_bytes(int64_t R, int64_t heads, int64_t H);
  *                                                  (the residual stream updated
  *                                                  in place), else disjoint
  *   out      [M x N] bf16                          (output)
- * out = RNE_bf16(act(a w^T + bias) + residual), the sum of lacache_linear_bf16
- * (fp32, the same bits) and the rest in fp32, one rounding at the end:
+ * out = RNE_bf16(act(a w^T + bias) + residual), all in fp32 with one rounding at
+ * the end; the sum is that of lacache_linear_bf16 bit for bit up to 128 rows, and
+ * one chain over K above (a row's result does not depend on M on either side):
  *   NONE x; RELU max(x, 0); SILU x / (1 + e^-x); GELU x (1 + erf(x / sqrt 2)) / 2
  *   (off by at most 0.75e-7 |x| before the rounding); GELU_TANH x (1 +
  *   tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
@@ -455,6 +456,9 @@ enum {
 };
 int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
+/* Test hook: the tile (activation rows, weight rows) that a workgroup of such a
+ * call takes on the current device. M > 0. Launches nothing. */
+int lacache_linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile);
 
 /*
  * Paged key/value cache: the keys and values of finished tokens (the prompt,

@@ -440,6 +440,13 @@ def lacache_linear_tile(M, N, K):
     return tile[0], tile[1]
 
 
+def lacache_linear_act_tile(M, N, K, act=LACACHE_ACT_NONE):
+    """(activation rows, weight rows) of the tiles of lacache_linear_act_bf16 for a call of these sizes."""
+    tile = (ctypes.c_int * 2)()
+    check(lib().lacache_linear_act_tile(M, N, K, act, tile), "lacache_linear_act_tile")
+    return tile[0], tile[1]
+
+
 def lacache_status_string(status):
     return status_string(status)
 

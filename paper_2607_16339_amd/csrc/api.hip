@@ -677,6 +677,18 @@ int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, 
   return hip_status(launch_linear_act(static_cast<hipStream_t>(stream), a, w, bias, residual, out, M, N, K, act));
 }
 
+int lacache_linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile) {
+  if (act < LACACHE_ACT_NONE || act > LACACHE_ACT_SWIGLU) return LACACHE_ERR_INVALID_ARG;
+  RETURN_IF(check_m(M));
+  RETURN_IF(check_dim(N, kMaxN));
+  RETURN_IF(check_dim(K, kMaxN));
+  if (M == 0 || tile == nullptr) return LACACHE_ERR_INVALID_ARG;
+  int t[2];
+  linear_act_tile(M, N, K, act, t);
+  std::memcpy(tile, t, sizeof(t));
+  return LACACHE_OK;
+}
+
 int lacache_linear_tile(int64_t M, int64_t N, int64_t K, int* tile) {
   RETURN_IF(check_m(M));
   RETURN_IF(check_dim(N, kMaxN));

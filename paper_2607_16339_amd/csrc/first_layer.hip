@@ -25,8 +25,8 @@
 // the device (no access is made for them).
 #include <type_traits>
 
+#include "activation.h"
 #include "device.h"
-#include "lacache.h"
 #include "launch.h"
 
 namespace lacache {
@@ -136,11 +136,6 @@ __device__ __forceinline__ uint16_t* rope_dst(const RopeArgs& ra, int head) {
 // weight rows n (gate) and N + n (up), which meet in one wavefront as a pair of
 // kRope does. The sums before the epilogue are kPlain's, bit for bit.
 constexpr int kPlain = 0, kRope = 1, kAct = 2, kSwiGlu = 3;
-struct ActArgs {
-  const uint16_t* bias;      // [weight rows], nullable
-  const uint16_t* residual;  // [M x N], nullable; may be the output
-  int act;                   // kAct: a LACACHE_ACT_ value
-};
 template <int kEpi>
 struct EpiOf {
   using Args = RopeArgs;
@@ -155,39 +150,6 @@ struct EpiOf<kSwiGlu> {
 };
 template <int kEpi>
 using EpiArgs = typename EpiOf<kEpi>::Args;
-
-// exp(-x) and 1 / x by the hardware's exp2 and reciprocal (1 ulp each).
-__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
-__device__ __forceinline__ float silu(float x) { return x * fast_rcp(1.0f + exp_neg(x)); }
-// gelu(x) = x Phi(x), Phi(x) = erfc(-x / sqrt 2) / 2, with erfc(z), z >= 0, by formula
-// 7.1.26 of Abramowitz and Stegun (t = 1 / (1 + 0.3275911 z), t times a polynomial of
-// degree 4 in t, times exp(-z^2); off by at most 1.5e-7, so gelu by 0.75e-7 |x|): 13
-// instructions where the library's erfc takes several times that, and it is applied
-// to every output.
-__device__ __forceinline__ float gelu(float x) {
-  const float z = __builtin_fabsf(x) * 0.70710678118654752f;
-  const float t = fast_rcp(__builtin_fmaf(0.3275911f, z, 1.0f));
-  float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-  p = __builtin_fmaf(p, t, 1.421413741f);
-  p = __builtin_fmaf(p, t, -0.284496736f);
-  p = __builtin_fmaf(p, t, 0.254829592f);
-  const float e = 0.5f * p * t * exp_neg(z * z);  // erfc(z) / 2
-  return x * (x >= 0.0f ? 1.0f - e : e);
-}
-// 0.5 x (1 + tanh u) = x / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3)
-__device__ __forceinline__ float gelu_tanh(float x) {
-  const float u = 1.5957691216057308f * __builtin_fmaf(0.044715f * x * x, x, x);
-  return x * fast_rcp(1.0f + exp_neg(u));
-}
-__device__ __forceinline__ float activate(int act, float x) {
-  switch (act) {  // (the same for the whole call)
-    case LACACHE_ACT_RELU: return x < 0.0f ? 0.0f : x;
-    case LACACHE_ACT_SILU: return silu(x);
-    case LACACHE_ACT_GELU: return gelu(x);
-    case LACACHE_ACT_GELU_TANH: return gelu_tanh(x);
-    default: return x;
-  }
-}
 
 // The four bf16 values that this lane stored at p, NaNs as 0x7FC0.
 __device__ __forceinline__ void quiet_stored(uint2* p) {
@@ -371,7 +333,9 @@ __global__ __launch_bounds__(kLinSplit * 64) void linear_bf16_kernel(const uint1
     for (int wv = 1; wv < kLinSplit; ++wv) sum += red[(wv * RA + row) * NC + col];
     if constexpr (kEpi == kAct) {
       if (ra.bias != nullptr) sum += bf16lo(ra.bias[n0 + col]);
-      sum = activate(ra.act, sum);
+      float v[1] = {sum};
+      activate(ra.act, v);
+      sum = v[0];
       if (ra.residual != nullptr) sum += bf16lo(ra.residual[(m0 + row) * N + n0 + col]);
     }
     out[(m0 + row) * N + n0 + col] = static_cast<uint16_t>(sum == sum ? cvt_pk_bf16(sum, 0.0f) : 0x7FC0u);
@@ -410,15 +374,14 @@ constexpr int kLtWaves = 8;
 constexpr int64_t kLinTiledMinM = LACACHE_LIN_TILED_MIN_M;  // rows above which the tiled kernel runs
 
 // kRope: a wavefront's NT slabs are NT/2 slabs of 16 pairs' lower rows, then
-// the same pairs' upper rows (weight rows 64 on; kSwiGlu: N/2 on).
-template <int BM, int BN, bool kPing, int kEpi>
+// the same pairs' upper rows (weight rows 64 on).
+template <int BM, int BN, bool kPing, bool kRope>
 __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const uint16_t* __restrict__ a,
                                                                         const uint16_t* __restrict__ w,
                                                                         uint16_t* __restrict__ out,
                                                                         float* __restrict__ out_tap, int64_t M,
                                                                         int64_t N, int64_t K, int R, int C,
-                                                                        EpiArgs<kEpi> ra) {
-  constexpr bool kPair = kEpi == kRope || kEpi == kSwiGlu;
+                                                                        RopeArgs ra) {
   constexpr int kA = BM * 128, kB = BN * 128;  // bytes of a K-step's activation and weight rows
   // steps in the two rings (a power of two of activations): 4 and 4, or 2 and 4 at 256 x 192
   constexpr int DA = 4 * (kA + kB) <= 163840 ? 4 : 2;
@@ -427,9 +390,8 @@ __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const 
   constexpr int PA = BM / 32, PB = BN / 32;  // copies per step of an activation / a weight copy wavefront
   constexpr int PM = PA > PB ? PA : PB;
   static_assert(BM % 64 == 0 && BN % 32 == 0 && DB >= 3, "tile shape");
-  __shared__ __align__(16) uint8_t ring[DA * kA + DB * kB];
-  uint8_t(*const sA)[kA] = reinterpret_cast<uint8_t(*)[kA]>(ring);
-  uint8_t(*const sB)[kB] = reinterpret_cast<uint8_t(*)[kB]>(ring + DA * kA);
+  __shared__ __align__(16) uint8_t sA[DA][kA];
+  __shared__ __align__(16) uint8_t sB[DB][kB];
   const int t = threadIdx.x, lane = t & 63;
   const int wave = wave_uniform(t >> 6);
   const int q = lane >> 4, lr = lane & 15;
@@ -451,21 +413,19 @@ __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const 
     xcd_grouped_tile(item, R, C, rt, ct);
     const int64_t m0 = static_cast<int64_t>(rt) * BM, n0 = static_cast<int64_t>(ct) * BN;
     // rows past M fetch the last row; their results are never stored
-    const uint8_t* base = late ? reinterpret_cast<const uint8_t*>(kPair ? w : w + n0 * K)
+    const uint8_t* base = late ? reinterpret_cast<const uint8_t*>(kRope ? w : w + n0 * K)
                                : reinterpret_cast<const uint8_t*>(a + m0 * K);
     const int64_t last = late ? BN - 1 : (M - 1 - m0 < BM - 1 ? M - 1 - m0 : BM - 1);
-    const uint32_t lim = late && kPair ? 0xFFFFFFFFu : static_cast<uint32_t>(last) * K2;
-    // byte offset of copy u's 8 rows from the first copy's (kPair: weight rows
+    const uint32_t lim = late && kRope ? 0xFFFFFFFFu : static_cast<uint32_t>(last) * K2;
+    // byte offset of copy u's 8 rows from the first copy's (kRope: weight rows
     // by pair slab; below 2^32, as N K < 2^31)
-    uint32_t uoff[kPair ? PM : 1];
-    if (kPair) {
+    uint32_t uoff[kRope ? PM : 1];
+    if (kRope) {
 #pragma unroll
       for (int u = 0; u < PM; ++u) {
         const int g = (wave & 3) + 4 * u, slab = g >> 1, j = slab % NT;
         const int ps = ct * (BN / 32) + (slab / NT) * (NT / 2) + j % (NT / 2);
-        const int row = (kEpi == kRope ? (ps >> 2) * 128 + (ps & 3) * 16 + (j < NT / 2 ? 0 : 64)
-                                       : ps * 16 + (j < NT / 2 ? 0 : static_cast<int>(N / 2))) +
-                        8 * (g & 1);
+        const int row = (ps >> 2) * 128 + (ps & 3) * 16 + (j < NT / 2 ? 0 : 64) + 8 * (g & 1);
         uoff[u] = late ? static_cast<uint32_t>(row - 8 * (wave & 3)) * K2 : static_cast<uint32_t>(32 * u) * K2;
       }
     }
@@ -476,7 +436,7 @@ __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const 
       const uint8_t* g = base + static_cast<int64_t>(ks < KS ? ks : KS - 1) * 128;
 #pragma unroll
       for (int u = 0; u < P; ++u) {
-        const uint32_t o = coff + (kPair ? uoff[kPair ? u : 0] : static_cast<uint32_t>(32 * u) * K2);
+        const uint32_t o = coff + (kRope ? uoff[kRope ? u : 0] : static_cast<uint32_t>(32 * u) * K2);
         dma16s(g, (o < lim ? o : lim) + cchunk, wave_uniform(lds + u * 4096));
       }
     };
@@ -570,7 +530,7 @@ __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const 
     if (kPing && !late) bar();
     wait_vm<0>();  // the trailing repeat copies
     bar();         // every wavefront is done with the ring: the next item may refill it
-    if constexpr (kEpi == kRope) {
+    if (kRope) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t row = m0 + 16 * (MT * wm + i) + lr;
@@ -622,69 +582,6 @@ __global__ __launch_bounds__(kLtWaves * 64) void linear_bf16_tiled_kernel(const 
         }
       }
       continue;  // the next item
-    }
-    if constexpr (kEpi == kAct || kEpi == kSwiGlu) {
-      // The wavefront's sums go through its part of the idle ring, half of its rows at a
-      // time, so that the epilogue is one short loop (its activations inlined once) and
-      // reads the residual and writes the output 16 bytes a lane, 8 NT or 16 NT columns
-      // (at least 64 bytes) of a row together.
-      constexpr int kCols = 16 * NT, kPitch = kCols + 4;  // fp32; 4: rows apart by 16 bytes of the banks
-      constexpr int kOut = kEpi == kSwiGlu ? kCols / 2 : kCols, kVec = kOut / 8, kRows = 8 * MT;
-      static_assert(kLtWaves * kRows * kPitch * 4 <= DA * kA + DB * kB && MT % 2 == 0 && kOut % 8 == 0, "epilogue tile");
-      float* const tile = reinterpret_cast<float*>(ring) + wave * kRows * kPitch;
-      const int64_t no = kEpi == kSwiGlu ? N / 2 : N;
-      const int64_t colw = (kEpi == kSwiGlu ? n0 / 2 : n0) + kOut * wn;
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-#pragma unroll
-        for (int i = 0; i < MT / 2; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            *reinterpret_cast<v4f*>(tile + (16 * i + lr) * kPitch + 16 * j + 4 * q) = tot[part * (MT / 2) + i][j];
-        wait_lds();
-        asm volatile("" ::: "memory");
-        for (int e = lane; e < kRows * kVec; e += 64) {
-          const int rr = e / kVec, c8 = 8 * (e - rr * kVec);
-          const int64_t row = m0 + 16 * MT * wm + part * kRows + rr;
-          if (row >= M) break;  // (so are this lane's later ones)
-          const float* src = tile + rr * kPitch + c8;
-          const int64_t col = colw + c8, at = row * no + col;
-          uint4 bv = make_uint4(0u, 0u, 0u, 0u), b2 = bv, rv = bv;
-          if (ra.bias != nullptr) {
-            bv = *reinterpret_cast<const uint4*>(ra.bias + col);
-            if (kEpi == kSwiGlu) b2 = *reinterpret_cast<const uint4*>(ra.bias + no + col);
-          }
-          if (ra.residual != nullptr) rv = *reinterpret_cast<const uint4*>(ra.residual + at);
-          const uint32_t bw[4] = {bv.x, bv.y, bv.z, bv.w}, cw[4] = {b2.x, b2.y, b2.z, b2.w};
-          const uint32_t rw[4] = {rv.x, rv.y, rv.z, rv.w};
-          uint32_t ow[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float y[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float v = src[2 * x + k];
-              if (ra.bias != nullptr) v += k ? bf16hi(bw[x]) : bf16lo(bw[x]);
-              if (kEpi == kSwiGlu) {
-                float u = src[kOut + 2 * x + k];
-                if (ra.bias != nullptr) u += k ? bf16hi(cw[x]) : bf16lo(cw[x]);
-                v = silu(v) * u;
-              } else {
-                v = activate(ra.act, v);
-              }
-              if (ra.residual != nullptr) v += k ? bf16hi(rw[x]) : bf16lo(rw[x]);
-              y[k] = v;
-            }
-            ow[x] = cvt_pk_bf16(y[0], y[1]);
-            if (__builtin_isunordered(y[0], y[1])) ow[x] = bf16x2_quiet(ow[x]);
-          }
-          *reinterpret_cast<uint4*>(out + at) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
-        }
-        wait_lds();
-        asm volatile("" ::: "memory");
-      }
-      bar();  // the next item's copies overwrite the ring
-      continue;
     }
     const int64_t col0 = n0 + 16 * NT * wn + 4 * q;
 #pragma unroll
@@ -808,27 +705,8 @@ LinTile lin_tile(int64_t M, int64_t N, int64_t K) {
 bool lin_wide(int64_t M, int64_t N) { return M <= 32 && N % 48 == 0 && N / 48 >= 256; }
 
 template <int kEpi>
-hipError_t launch_linear(hipStream_t st, const uint16_t* a, const uint16_t* w, uint16_t* out, float* out_tap, int64_t M,
-                         int64_t N, int64_t K, const EpiArgs<kEpi>& ra) {
-  if (M > kLinTiledMinM) {
-    const LinTile tile = lin_tile(M, N, K);
-    const int64_t cus = device_cu_count();
-#define LT(BM_, BN_, PING_)                                                                                       \
-  do {                                                                                                           \
-    const int r_ = static_cast<int>((M + BM_ - 1) / BM_), c_ = static_cast<int>(N / BN_);                        \
-    hipLaunchKernelGGL((linear_bf16_tiled_kernel<BM_, BN_, PING_, kEpi>),                                               \
-                       dim3(static_cast<unsigned>(static_cast<int64_t>(r_) * c_ < cus ? r_ * c_ : cus)),         \
-                       dim3(kLtWaves * 64), 0, st, a, w, out, out_tap, M, N, K, r_, c_, ra);                         \
-  } while (0)
-    if (tile.bm == 256)
-      LT(256, 192, true);
-    else if (tile.bn == 192)
-      LT(128, 192, false);
-    else
-      LT(128, 128, false);
-#undef LT
-    return hipGetLastError();
-  }
+hipError_t launch_linear_rows(hipStream_t st, const uint16_t* a, const uint16_t* w, uint16_t* out, float* out_tap,
+                              int64_t M, int64_t N, int64_t K, const EpiArgs<kEpi>& ra) {
   // up to 64 rows per pass; the last pass may hold fewer slabs
   const unsigned passes = static_cast<unsigned>((M + 63) / 64);
   const int mt = static_cast<int>(M >= 64 ? 4 : (M + 15) / 16);
@@ -846,6 +724,31 @@ hipError_t launch_linear(hipStream_t st, const uint16_t* a, const uint16_t* w, u
   return hipGetLastError();
 }
 
+template <bool kRope>
+hipError_t launch_linear(hipStream_t st, const uint16_t* a, const uint16_t* w, uint16_t* out, float* out_tap, int64_t M,
+                         int64_t N, int64_t K, const RopeArgs& ra) {
+  if (M > kLinTiledMinM) {
+    const LinTile tile = lin_tile(M, N, K);
+    const int64_t cus = device_cu_count();
+#define LT(BM_, BN_, PING_)                                                                                       \
+  do {                                                                                                           \
+    const int r_ = static_cast<int>((M + BM_ - 1) / BM_), c_ = static_cast<int>(N / BN_);                        \
+    hipLaunchKernelGGL((linear_bf16_tiled_kernel<BM_, BN_, PING_, kRope>),                                              \
+                       dim3(static_cast<unsigned>(static_cast<int64_t>(r_) * c_ < cus ? r_ * c_ : cus)),         \
+                       dim3(kLtWaves * 64), 0, st, a, w, out, out_tap, M, N, K, r_, c_, ra);                         \
+  } while (0)
+    if (tile.bm == 256)
+      LT(256, 192, true);
+    else if (tile.bn == 192)
+      LT(128, 192, false);
+    else
+      LT(128, 128, false);
+#undef LT
+    return hipGetLastError();
+  }
+  return launch_linear_rows<kRope ? lacache::kRope : kPlain>(st, a, w, out, out_tap, M, N, K, ra);
+}
+
 }  // namespace
 
 void linear_tile(int64_t M, int64_t N, int64_t K, int (&tile)[2]) {
@@ -859,20 +762,21 @@ void linear_tile(int64_t M, int64_t N, int64_t K, int (&tile)[2]) {
 
 hipError_t launch_linear_bf16(hipStream_t st, const uint16_t* a, const uint16_t* w, uint16_t* out, float* out_tap,
                               int64_t M, int64_t N, int64_t K) {
-  return launch_linear<kPlain>(st, a, w, out, out_tap, M, N, K, RopeArgs{});
+  return launch_linear<false>(st, a, w, out, out_tap, M, N, K, RopeArgs{});
 }
 
-hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
-                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {
-  const ActArgs aa{bias, residual, act};
-  if (act == LACACHE_ACT_SWIGLU) return launch_linear<kSwiGlu>(st, a, w, out, nullptr, M, 2 * N, K, aa);
-  return launch_linear<kAct>(st, a, w, out, nullptr, M, N, K, aa);
+bool linear_streams_rows(int64_t M) { return M <= kLinTiledMinM; }
+
+hipError_t launch_linear_act_rows(hipStream_t st, const uint16_t* a, const uint16_t* w, const ActArgs& act, uint16_t* out,
+                                  int64_t M, int64_t N, int64_t K) {
+  if (act.act == LACACHE_ACT_SWIGLU) return launch_linear_rows<kSwiGlu>(st, a, w, out, nullptr, M, 2 * N, K, act);
+  return launch_linear_rows<kAct>(st, a, w, out, nullptr, M, N, K, act);
 }
 
 hipError_t launch_linear_rope(hipStream_t st, const uint16_t* y, const uint16_t* w_qkv, const int32_t* rows, int64_t R,
                               const float* cs, const float* sn, uint16_t* q, uint16_t* k, uint16_t* v, int64_t heads,
                               int64_t N, int64_t H) {
-  return launch_linear<kRope>(st, y, w_qkv, nullptr, nullptr, R, 3 * heads * 128, H,
+  return launch_linear<true>(st, y, w_qkv, nullptr, nullptr, R, 3 * heads * 128, H,
                              RopeArgs{rows, cs, sn, q, k, v, static_cast<int>(heads), N});
 }
 

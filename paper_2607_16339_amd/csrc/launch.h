@@ -116,6 +116,13 @@ void linear_tile(int64_t M, int64_t N, int64_t K, int (&tile)[2]);
 // residual); act is a LACACHE_ACT_ value, SWIGLU with w [2N x K], bias [2N].
 hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
+// The tile of the call above: activation rows and weight rows of a workgroup.
+void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]);
+// The same for the few rows (linear_streams_rows) of the weight-streaming kernel.
+struct ActArgs;
+bool linear_streams_rows(int64_t M);
+hipError_t launch_linear_act_rows(hipStream_t st, const uint16_t* a, const uint16_t* w, const ActArgs& act, uint16_t* out,
+                                  int64_t M, int64_t N, int64_t K);
 // q, k, v rows of RoPE(y w_qkv^T) (rows [R], w_qkv [3 heads 128 x H]): the
 // bytes of launch_linear_bf16 followed by launch_rope_scatter, in one kernel.
 hipError_t launch_linear_rope(hipStream_t st, const uint16_t* y, const uint16_t* w_qkv, const int32_t* rows, int64_t R,

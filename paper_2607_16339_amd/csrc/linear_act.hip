@@ -1,0 +1,425 @@
+// The bf16 projection with its epilogue for many rows: out = act(a W^T + bias) +
+// residual, or silu(gate) up of two products (kGlu: weight rows n and Nw/2 + n,
+// which a wavefront holds as slabs of 16 gate rows and the same 16 up rows).
+// (Up to 128 rows the weight-streaming kernel of the first layer runs with the
+// same epilogue.)
+//
+// Each output is one chain of 16x16x32 bf16 MFMAs over K in order, whatever the
+// tile, so a row's result does not depend on M among these calls.
+//
+// K-steps of 64 elements (128 bytes of a row) come by direct copies into an LDS
+// ring, [rows][128 B] with the 16-byte chunk c of row r at c ^ ((r / 2) mod 8):
+// the 16 rows of an operand read touch every bank once. Rows past M and columns
+// past the weight's rows fetch the last one and are not stored.
+#include "activation.h"
+#include "device.h"
+#include "launch.h"
+
+namespace lacache {
+namespace {
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+
+struct LinCall {
+  const uint16_t* a;
+  const uint16_t* w;
+  uint16_t* out;
+  ActArgs act;
+  int64_t M, K;
+  int64_t Nw;  // weight rows
+  int R, C;    // row and column tiles
+};
+
+// Copies of the rows of a K-step: copy u of wavefront v of W fills rows 8 (v + W u) ..
+// of the tile's activation or weight rows, lane l row l / 8, chunk (l mod 8) ^ swizzle.
+struct CopyPlan {
+  int crow;
+  uint32_t chunk;  // of even groups of 8 rows; odd ones flip bit 6
+};
+__device__ __forceinline__ CopyPlan copy_plan(int lane) {
+  return {lane >> 3, static_cast<uint32_t>(((lane & 7) ^ (lane >> 4)) << 4)};
+}
+// Byte offset from a (row 0 of the tile) of the lane's chunk of rows 8 g ..; last: the last row that exists.
+__device__ __forceinline__ uint32_t row_off(const CopyPlan& p, int g, uint32_t K2, int64_t last) {
+  const int row = 8 * g + p.crow;
+  return static_cast<uint32_t>(row < last ? row : last) * K2 + (p.chunk ^ ((g & 1) << 6));
+}
+// The weight row of row 8 g + r of a tile of BN rows from column tile ct (kGlu: bands of
+// 16 NT rows, NT/2 slabs of gate rows and then the up rows of the same columns).
+template <bool kGlu, int BN, int NT>
+__device__ __forceinline__ int64_t weight_row(int64_t Nw, int ct, int row) {
+  if (!kGlu) {
+    const int64_t n = static_cast<int64_t>(ct) * BN + row;
+    return n < Nw ? n : Nw - 1;
+  }
+  const int slab = row >> 4, j = slab % NT;
+  const int64_t n = static_cast<int64_t>(ct) * (BN / 2) + ((slab / NT) * (NT / 2) + j % (NT / 2)) * 16 + (row & 15);
+  return (n < Nw / 2 ? n : Nw / 2 - 1) + (j < NT / 2 ? 0 : Nw / 2);
+}
+
+// The sums acc[MT][NT] of a wavefront (rows row0 .., band of 16 NT weight rows wn of
+// column tile ct) to the output, through LDS of the wavefront's own, kSlabs slabs of
+// 16 rows at a time, so that the residual is read and the output written 16 bytes a
+// lane, a row's columns together. A lane keeps its 8 columns; the residual's loads
+// of a part are all in flight before its sums go through LDS, and the activation is
+// chosen once per 8 values (chosen per value, with a load between, a 256 x 256 tile's
+// epilogue took 18 us).
+template <bool kGlu, int BN, int MT, int NT, int kSlabs>
+struct Epilogue {
+  static constexpr int kCols = 16 * NT, kPitch = kCols + 4;  // fp32; 4: rows apart by 16 bytes of the banks
+  static constexpr int kRows = 16 * kSlabs, kBytes = kRows * kPitch * 4;
+  static constexpr int kOut = kGlu ? kCols / 2 : kCols, kVec = kOut / 8, kIters = (kRows * kVec + 63) / 64;
+  static_assert(MT % kSlabs == 0 && kOut % 8 == 0 && 64 % kVec == 0, "epilogue");
+
+  static __device__ __forceinline__ void unpack(const uint16_t* p, float (&v)[8]) {
+    const uint4 w4 = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[2 * x] = bf16lo(w[x]), v[2 * x + 1] = bf16hi(w[x]);
+  }
+  static __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const v4f a = *reinterpret_cast<const v4f*>(p), b = *reinterpret_cast<const v4f*>(p + 4);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = a[x], v[4 + x] = b[x];
+  }
+
+  static __device__ __forceinline__ void store(const LinCall& c, const v4f (&acc)[MT][NT], float* tile, int64_t row0,
+                                               int ct, int wn, int lane) {
+    const int q = lane >> 4, lr = lane & 15;
+    const int64_t no = kGlu ? c.Nw / 2 : c.Nw;
+    const int rl = lane / kVec, c8 = 8 * (lane % kVec);  // this lane's first row and its columns
+    const int64_t col = static_cast<int64_t>(ct) * (kGlu ? BN / 2 : BN) + kOut * wn + c8;
+    const bool bias = c.act.bias != nullptr && col < no;
+    float b1[8] = {}, b2[8] = {};
+    if (bias) {
+      unpack(c.act.bias + col, b1);
+      if (kGlu) unpack(c.act.bias + no + col, b2);
+    }
+#pragma unroll
+    for (int part = 0; part < MT / kSlabs; ++part) {
+      uint4 res[kIters];
+      bool live[kIters];
+#pragma unroll
+      for (int it = 0; it < kIters; ++it) {
+        const int rr = rl + it * (64 / kVec);
+        const int64_t row = row0 + part * kRows + rr;
+        live[it] = rr < kRows && row < c.M && col < no;
+        res[it] = make_uint4(0u, 0u, 0u, 0u);
+        if (c.act.residual != nullptr && live[it])
+          res[it] = *reinterpret_cast<const uint4*>(c.act.residual + row * no + col);
+      }
+#pragma unroll
+      for (int i = 0; i < kSlabs; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          *reinterpret_cast<v4f*>(tile + (16 * i + lr) * kPitch + 16 * j + 4 * q) = acc[part * kSlabs + i][j];
+      wait_lds();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int it = 0; it < kIters; ++it) {
+        if (!live[it]) continue;
+        const int rr = rl + it * (64 / kVec);
+        const float* src = tile + rr * kPitch + c8;
+        float v[8];
+        load8(src, v);
+        if (bias) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] += b1[x];
+        }
+        if (kGlu) {
+          float u[8];
+          load8(src + kOut, u);
+          if (bias) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) u[x] += b2[x];
+          }
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] = silu(v[x]) * u[x];
+        } else {
+          activate(c.act.act, v);
+        }
+        if (c.act.residual != nullptr) {
+          const uint32_t rw[4] = {res[it].x, res[it].y, res[it].z, res[it].w};
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] += x & 1 ? bf16hi(rw[x >> 1]) : bf16lo(rw[x >> 1]);
+        }
+        uint32_t ow[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          ow[x] = cvt_pk_bf16(v[2 * x], v[2 * x + 1]);
+          if (__builtin_isunordered(v[2 * x], v[2 * x + 1])) ow[x] = bf16x2_quiet(ow[x]);
+        }
+        *reinterpret_cast<uint4*>(c.out + (row0 + part * kRows + rr) * no + col) = make_uint4(ow[0], ow[1], ow[2], ow[3]);
+      }
+      wait_lds();
+      asm volatile("" ::: "memory");
+    }
+  }
+};
+
+// WR x WC wavefronts, each MT x NT slabs of a BM x BN tile, a ring of S steps.
+template <bool kGlu, int BM, int BN, int WR, int WC, int S>
+__global__ __launch_bounds__(64 * WR * WC) void linear_act_tile_kernel(LinCall c) {
+  constexpr int W = WR * WC, MT = BM / WR / 16, NT = BN / WC / 16, kStep = (BM + BN) * 128;
+  constexpr int PA = BM / 8 / W, PB = BN / 8 / W, P = PA + PB;
+  using Epi = Epilogue<kGlu, BN, MT, NT, 1>;
+  static_assert(BM % (8 * W) == 0 && BN % (8 * W) == 0 && S >= 3 && W * Epi::kBytes <= S * kStep && S * kStep <= 163840,
+                "tile shape");
+  __shared__ __align__(16) uint8_t ring[S * kStep];
+  const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
+  const int q = lane >> 4, lr = lane & 15, wm = wave / WC, wn = wave % WC;
+  const int KS = static_cast<int>(c.K / 64);
+  const uint32_t K2 = static_cast<uint32_t>(c.K) * 2u;
+  int rt, ct;
+  xcd_grouped_tile(static_cast<int>(blockIdx.x), c.R, c.C, rt, ct);
+  const int64_t m0 = static_cast<int64_t>(rt) * BM;
+  const CopyPlan cp = copy_plan(lane);
+  uint32_t ao[PA], bo[PB];
+#pragma unroll
+  for (int u = 0; u < PA; ++u) ao[u] = row_off(cp, wave + W * u, K2, c.M - 1 - m0);
+#pragma unroll
+  for (int u = 0; u < PB; ++u) {
+    const int g = wave + W * u;
+    bo[u] = static_cast<uint32_t>(weight_row<kGlu, BN, NT>(c.Nw, ct, 8 * g + cp.crow) -
+                                  (kGlu ? 0 : static_cast<int64_t>(ct) * BN)) * K2 + (cp.chunk ^ ((g & 1) << 6));
+  }
+  const uint8_t* ab = reinterpret_cast<const uint8_t*>(c.a + m0 * c.K);
+  const uint8_t* wb = reinterpret_cast<const uint8_t*>(kGlu ? c.w : c.w + static_cast<int64_t>(ct) * BN * c.K);
+  const uint32_t lds = lds_u32(ring);
+  auto issue = [&](int ks, int slot) {
+    // (past the end the last step again, never read)
+    const int64_t kb = static_cast<int64_t>(ks < KS ? ks : KS - 1) * 128;
+    const uint32_t dst = lds + slot * kStep;
+#pragma unroll
+    for (int u = 0; u < PA; ++u) dma16s(ab + kb, ao[u], wave_uniform(static_cast<int>(dst + (wave + W * u) * 1024)));
+#pragma unroll
+    for (int u = 0; u < PB; ++u)
+      dma16s(wb + kb, bo[u], wave_uniform(static_cast<int>(dst + BM * 128 + (wave + W * u) * 1024)));
+  };
+  const int frag[2] = {lr * 128 + ((q ^ (lr >> 1)) << 4), lr * 128 + (((4 + q) ^ (lr >> 1)) << 4)};
+  bf8 af[2][MT], bf[2][NT];
+  auto read = [&](int slot, int h) {
+    const uint8_t* pa = ring + slot * kStep + MT * wm * 2048 + frag[h];
+    const uint8_t* pb = ring + slot * kStep + BM * 128 + NT * wn * 2048 + frag[h];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) af[h][i] = *reinterpret_cast<const bf8*>(pa + i * 2048);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) bf[h][j] = *reinterpret_cast<const bf8*>(pb + j * 2048);
+  };
+  v4f acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  auto multiply = [&](int h) {
+    // weight rows first: a lane's four results are four consecutive columns of one row
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[h][j], af[h][i], acc[i][j], 0, 0, 0);
+  };
+
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) issue(s, s);
+  wait_vm<(S - 2) * P>();
+  bar();
+  read(0, 0);
+  int cur = 0;
+  for (int ks = 0; ks < KS; ++ks) {
+    const int nxt = cur + 1 == S ? 0 : cur + 1;
+    __builtin_amdgcn_sched_barrier(0);
+    read(cur, 1);
+    multiply(0);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm<(S - 3) * P>();  // this wavefront's copies of the next step have landed ...
+    bar();                   // ... and everyone's; step ks - 1 has been read
+    issue(ks + S - 1, cur == 0 ? S - 1 : cur - 1);
+    read(nxt, 0);
+    multiply(1);
+    cur = nxt;
+  }
+  wait_vm<0>();
+  bar();
+  Epi::store(c, acc, reinterpret_cast<float*>(ring + wave * Epi::kBytes), m0 + 16 * MT * wm, ct, wn, lane);
+}
+
+// 256 x 256 tiles, 8 wavefronts of 64 x 128, walked by at most one workgroup per CU.
+// Two wavefronts share a SIMD and alternate: one reads its operands and issues
+// copies while the other multiplies, a barrier between the phases. Wavefronts 0-3
+// copy the activation rows (ring of 2 steps), 4-7 the weight rows (of 3).
+template <bool kGlu>
+__global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
+  constexpr int BM = 256, BN = 256, MT = 4, NT = 8, kA = BM * 128, kB = BN * 128, DA = 2, DB = 3, P = 8;
+  using Epi = Epilogue<kGlu, BN, MT, NT, 2>;
+  static_assert(DA * kA + DB * kB <= 163840 && 8 * Epi::kBytes <= DA * kA + DB * kB, "tile shape");
+  __shared__ __align__(16) uint8_t ring[DA * kA + DB * kB];
+  uint8_t* const sB = ring + DA * kA;
+  const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
+  const int q = lane >> 4, lr = lane & 15, wm = wave >> 1, wn = wave & 1;
+  const bool late = wave >= 4;  // copies weights, half a phase behind the others
+  const int KS = static_cast<int>(c.K / 64);
+  const uint32_t K2 = static_cast<uint32_t>(c.K) * 2u;
+  const CopyPlan cp = copy_plan(lane);
+  const int frag[2] = {lr * 128 + ((q ^ (lr >> 1)) << 4), lr * 128 + (((4 + q) ^ (lr >> 1)) << 4)};
+
+  for (int item = blockIdx.x; item < c.R * c.C; item += gridDim.x) {
+    int rt, ct;
+    xcd_grouped_tile(item, c.R, c.C, rt, ct);
+    const int64_t m0 = static_cast<int64_t>(rt) * BM;
+    const uint8_t* base = late ? reinterpret_cast<const uint8_t*>(kGlu ? c.w : c.w + static_cast<int64_t>(ct) * BN * c.K)
+                               : reinterpret_cast<const uint8_t*>(c.a + m0 * c.K);
+    uint32_t off[P];
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      const int g = (wave & 3) + 4 * u;
+      const uint32_t x = cp.chunk ^ ((g & 1) << 6);
+      off[u] = late ? static_cast<uint32_t>(weight_row<kGlu, BN, NT>(c.Nw, ct, 8 * g + cp.crow) -
+                                            (kGlu ? 0 : static_cast<int64_t>(ct) * BN)) * K2 + x
+                    : row_off(cp, g, K2, c.M - 1 - m0);
+    }
+    auto issue = [&](int ks, uint8_t* dst) {
+      const uint8_t* g = base + static_cast<int64_t>(ks < KS ? ks : KS - 1) * 128;
+      const int l = static_cast<int>(lds_u32(dst)) + (wave & 3) * 1024;
+#pragma unroll
+      for (int u = 0; u < P; ++u) dma16s(g, off[u], wave_uniform(l + u * 4096));
+    };
+    auto landed = [&]() {
+      if (late)
+        wait_vm<(DB - 2) * P>();
+      else
+        wait_vm<(DA - 2) * P>();
+    };
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (late) {
+      issue(0, sB);
+      issue(1, sB + kB);
+    } else {
+      issue(0, ring);
+    }
+    landed();
+    bar();  // step 0 is in LDS
+    if (late) bar();
+    int cur = 0;
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t* pa = ring + (ks & 1) * kA + frag[h] + MT * wm * 2048;
+        const uint8_t* pb = sB + cur * kB + frag[h] + NT * wn * 2048;
+        bf8 af[MT], bf[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) af[i] = *reinterpret_cast<const bf8*>(pa + i * 2048);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) bf[j] = *reinterpret_cast<const bf8*>(pb + j * 2048);
+        if (h == 0) {  // into the stages of step ks - 1, which every wavefront has read
+          if (late)
+            issue(ks + DB - 1, sB + (cur == 0 ? DB - 1 : cur - 1) * kB);
+          else
+            issue(ks + DA - 1, ring + ((ks + 1) & 1) * kA);
+        }
+        if (h == 1 && late) landed();
+        wait_lds();
+        bar();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (h == 1 && !late) landed();
+        bar();
+      }
+      cur = cur + 1 == DB ? 0 : cur + 1;
+    }
+    if (!late) bar();
+    wait_vm<0>();  // the trailing repeat copies
+    bar();         // every wavefront is done with the ring
+    Epi::store(c, acc, reinterpret_cast<float*>(ring + wave * Epi::kBytes), m0 + 16 * MT * wm, ct, wn, lane);
+    bar();  // the next item's copies overwrite the ring
+  }
+}
+
+// The tiles, and a call's time on each: rounds of one workgroup per CU of a start and
+// end and K/64 steps, and a step's time that grows with the work in flight. Fitted at
+// 152 sizes, M = 129..8192, N x K = 128 x 4096 to 24576 x 4096 and 16384 x 512, all
+// tiles in turn in one process: on average 0.24 % slower than the best tile, 8 % at
+// most (N = 16384, K = 512). At N = K = 4096, in us on 64 x 64, 64 x 128, 128 x 128,
+// 128 x 256 and 256 x 256: M = 200 17, 23, 32, 52, 88; 512 32, 25, 33, 53, 89; 1024
+// 60, 46, 37, 54, 91; 2048 125, 94, 73, 60, 97; 8192 511, 385, 293, 246, 206.
+// More wavefronts of less work each were better throughout: a step of a lone workgroup
+// is a chain of barrier, LDS reads and products (128 x 128 on 4, 8 and 16 wavefronts,
+// M = 512, N = K = 4096: 43, 36, 33).
+struct Shape {
+  int bm, bn;
+  double start, c0, c1;
+};
+constexpr Shape kShapes[5] = {{64, 64, 1.75, 0.130, 0.057},
+                              {64, 128, 1.87, 0.208, 0.097},
+                              {128, 128, 1.93, 0.304, 0.176},
+                              {128, 256, 2.28, 0.599, 0.315},
+                              {256, 256, 9.00, 1.032, 0.358}};
+
+int best_shape(int64_t M, int64_t Nw, int64_t K) {
+  const int64_t cus = device_cu_count();
+  const double ks = static_cast<double>(K) / 64.0;
+  int pick = 0;
+  double best = 0.0;
+  for (int t = 0; t < 5; ++t) {
+    const Shape& s = kShapes[t];
+    const int64_t items = ((M + s.bm - 1) / s.bm) * ((Nw + s.bn - 1) / s.bn);
+    const double rounds = static_cast<double>((items + cus - 1) / cus);
+    const double us = rounds * (s.start + s.c0 * ks) + s.c1 * ks * static_cast<double>(items) / static_cast<double>(cus);
+    if (t == 0 || us < best) pick = t, best = us;
+  }
+  return pick;
+}
+
+template <bool kGlu>
+hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
+  c.R = static_cast<int>((c.M + kShapes[shape].bm - 1) / kShapes[shape].bm);
+  c.C = static_cast<int>((c.Nw + kShapes[shape].bn - 1) / kShapes[shape].bn);
+  const int64_t items = static_cast<int64_t>(c.R) * c.C, cus = device_cu_count();
+  const dim3 all(static_cast<unsigned>(items)), round(static_cast<unsigned>(items < cus ? items : cus));
+#define LT(I_, WR_, WC_, S_)                                                                                             \
+  case I_:                                                                                                               \
+    hipLaunchKernelGGL((linear_act_tile_kernel<kGlu, kShapes[I_].bm, kShapes[I_].bn, WR_, WC_, S_>), all,                \
+                       dim3(64 * WR_ * WC_), 0, st, c);                                                                  \
+    break
+  switch (shape) {
+    LT(0, 4, 2, 8);
+    LT(1, 2, 4, 6);
+    LT(2, 4, 4, 5);
+    LT(3, 4, 4, 3);
+    default: hipLaunchKernelGGL((linear_act_256_kernel<kGlu>), round, dim3(512), 0, st, c);
+  }
+#undef LT
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
+                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {
+  const ActArgs aa{bias, residual, act};
+  if (linear_streams_rows(M)) return launch_linear_act_rows(st, a, w, aa, out, M, N, K);
+  const bool glu = act == LACACHE_ACT_SWIGLU;
+  LinCall c{a, w, out, aa, M, K, glu ? 2 * N : N, 0, 0};
+  const int shape = best_shape(M, c.Nw, K);
+  return glu ? launch_shape<true>(st, c, shape) : launch_shape<false>(st, c, shape);
+}
+
+void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]) {
+  const int64_t Nw = act == LACACHE_ACT_SWIGLU ? 2 * N : N;
+  if (linear_streams_rows(M)) return linear_tile(M, Nw, K, tile);
+  const Shape& s = kShapes[best_shape(M, Nw, K)];
+  tile[0] = s.bm, tile[1] = s.bn;
+}
+
+}  // namespace lacache

@@ -1,10 +1,11 @@
 """The bf16 product with bias, activation and residual, on the GPU.
 
-The sum before the epilogue is lacache_linear_bf16's (its fp32 tap, tested
-elsewhere against 64 bits), so the epilogue is checked in 64 bits on that very
-sum. Tolerance: the output's rounding 2^-8 |ref|, and before it the fp32 steps:
-x = sum + bias (u = 2^-24 relative to |x|, which an activation of slope at most
-1.13 passes on), the activation's hardware exp2 and reciprocal with the
+Up to 128 rows the sum before the epilogue is lacache_linear_bf16's (its fp32
+tap, tested elsewhere against 64 bits), so the epilogue is checked in 64 bits on
+that very sum; above, on the sum in 64 bits, off by the fp32 chain's K u sum|a w|
+(u = 2^-24). Tolerance: the output's rounding 2^-8 |ref|, and before it the fp32 steps:
+x = sum + bias (u relative to |x|, which with the sum's error an activation of slope
+at most 1.13 passes on), the activation's hardware exp2 and reciprocal with the
 rounding of its argument (|x| u + 8 u relative for SiLU's and tanh-GELU's
 exponential, whose cube adds 3 u |argument|), erf's formula (0.75e-7 |x|), SwiGLU's product
 and the residual's addition (u each)."""
@@ -22,9 +23,9 @@ U = 2.0 ** -24
 NONE, RELU, SILU, GELU, GELU_TANH, SWIGLU = range(6)
 
 
-def _act(act, x):
-    """(value, its tolerance) of the activation of x, which is off by u |x|."""
-    slack = 1.2 * U * x.abs()
+def _act(act, x, off):
+    """(value, its tolerance) of the activation of x, which is off by u |x| and `off`."""
+    slack = 1.2 * (U * x.abs() + off)
     if act == RELU:
         return x.clamp_min(0.0), slack
     if act in (SILU, SWIGLU):
@@ -50,17 +51,25 @@ def _case(M, N, K, act, bias, residual, seed=0, std=1.0):
 
 def _want(a, w, b, r, act):
     M, rows = a.shape[0], w.shape[0]
-    tap = torch.empty((M, rows), dtype=torch.float32, device=DEV)
-    lc.lacache_linear_bf16(a, w, torch.empty((M, rows), dtype=torch.bfloat16, device=DEV), tap)
-    x = tap.double() if b is None else tap.double() + b.double()
+    if M <= 128:
+        tap = torch.empty((M, rows), dtype=torch.float32, device=DEV)
+        lc.lacache_linear_bf16(a, w, torch.empty((M, rows), dtype=torch.bfloat16, device=DEV), tap)
+        x = tap.double()
+        off = torch.zeros_like(x)
+    else:
+        wt = w.double().t().contiguous()
+        x = a.double() @ wt
+        off = a.shape[1] * U * (a.double().abs() @ wt.abs())
+    if b is not None:
+        x = x + b.double()
     if act == SWIGLU:
         N = rows // 2
-        y, t = _act(SWIGLU, x[:, :N])
-        u = x[:, N:]
-        t = t * u.abs() + y.abs() * u.abs() * 3 * U
+        y, t = _act(SWIGLU, x[:, :N], off[:, :N])
+        u, du = x[:, N:], off[:, N:]
+        t = t * (u.abs() + du) + y.abs() * (u.abs() * 3 * U + du)
         y = y * u
     else:
-        y, t = _act(act, x)
+        y, t = _act(act, x, off)
     if r is not None:
         y = y + r.double()
         t = t + U * y.abs()
@@ -86,7 +95,7 @@ def _check(M, N, K, act, bias, residual, seed=0, std=1.0, in_place=False):
     return out
 
 
-# rows of every path: 1 to 4 slabs streamed, two passes, tiles of 128 and 256 rows, ragged ends
+# 1 to 4 slabs streamed, two passes, and tiles, with ragged ends
 ROWS = [1, 2, 16, 17, 32, 33, 48, 64, 65, 100, 128, 129, 200, 257, 1000]
 
 
@@ -118,7 +127,38 @@ def test_residual_updated_in_place(M, act):
     assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
-@pytest.mark.parametrize("M", [1, 64, 100, 300, 1500])
+# (M, N, K) of each tile; ragged rows, and columns where the tile is wider than what is left
+TILES = {(64, 64): [(130, 128, 256), (700, 1152, 640)], (64, 128): [(300, 4224, 512), (1500, 1152, 640)],
+         (128, 128): [(1000, 4096, 256), (1300, 2944, 512)], (128, 256): [(2047, 4096, 384), (2040, 3968, 1024)],
+         (256, 256): [(8000, 4096, 1024), (6000, 2176, 2048)]}
+
+
+@pytest.mark.parametrize("tile", sorted(TILES))
+@pytest.mark.parametrize("act", [NONE, GELU, SWIGLU])
+def test_tiles(tile, act):
+    for M, N, K in TILES[tile]:
+        if act == SWIGLU:
+            N = max(128, N // 2 // 128 * 128)
+        assert act == SWIGLU or lc.lacache_linear_act_tile(M, N, K, act) == tile
+        _check(M, N, K, act, True, True, seed=M + N)
+
+
+@pytest.mark.parametrize("act", [NONE, SWIGLU])
+def test_rows_do_not_depend_on_the_call(act):
+    """The first rows of calls of more than 128 rows, on every tile, are the same bytes."""
+    a, w, b, r = _case(8192, 1024, 1024, act, True, True, seed=3)
+    seen, first = set(), None
+    for M in (129, 200, 700, 1500, 3000, 8192):
+        out = torch.empty((M, 1024), dtype=torch.bfloat16, device=DEV)
+        lc.lacache_linear_act_bf16(a[:M], w, out, bias=b, residual=r[:M], act=act)
+        seen.add(lc.lacache_linear_act_tile(M, 1024, 1024, act))
+        first = out[:129].clone() if first is None else first
+        assert torch.equal(out[:129].view(torch.int16), first.view(torch.int16)), M
+    print(sorted(seen))
+    assert len(seen) >= 4
+
+
+@pytest.mark.parametrize("M", [1, 16, 33, 64, 100, 128])
 def test_no_epilogue_is_the_plain_product_bit_for_bit(M):
     a, w, _, _ = _case(M, 1152, 512, NONE, False, False, seed=M)
     a[0, 3] = float("nan")

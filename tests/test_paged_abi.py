@@ -119,6 +119,11 @@ def test_linear_act_refusals(L):
     # the gate and up rows: twice N
     assert _linear(L, act=5, out=_addr(2) + 256 * 128 * 2 + 4096) == INVALID
     assert _linear(L, M=0, act=5) == OK
+    import ctypes
+    t = (ctypes.c_int * 2)()
+    assert L.lacache_linear_act_tile(300, 256, 128, 0, t) == OK and tuple(t) in ((64, 64), (64, 128))
+    for bad in ((0, 256, 128, 0, t), (300, 100, 128, 0, t), (300, 256, 128, 6, t), (300, 256, 128, 0, None)):
+        assert L.lacache_linear_act_tile(*bad) == INVALID, bad
 
 
 def test_binding_refusals():
