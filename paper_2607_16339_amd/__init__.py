@@ -51,26 +51,18 @@ def _ptr(t, dtypes, name, shape=None, optional=False):
     return t.data_ptr()
 
 
-class _Stay:
-    def __enter__(self):
-        return None
-
-    def __exit__(self, *exc):
-        return False
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-_STAY = _Stay()
-
-
-def _on(first, *others):
-    """The context in which a call on these tensors runs: their device current (its workspace and
-    compute units are the current device's). Tensors of several devices are refused."""
-    dev = first.device
+def _elsewhere(first, *others):
+    """None where the tensors' device is current, else the context that makes it so (a call's
+    workspace and compute units are the current device's). Tensors of several devices are refused."""
+    dev = first.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("tensors on %s and %s" % (dev, t.device))
-    if not first.is_cuda or dev.index == torch.cuda.current_device():
-        return _STAY  # (a host tensor is refused by name in _ptr)
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors on %s and %s" % (first.device, t.device))
+    if dev < 0 or dev == _current_device():
+        return None  # (a host tensor is refused by name in _ptr)
     return torch.cuda.device(dev)
 
 
@@ -311,12 +303,14 @@ def lacache_linear_act_bf16(a, w, out, bias=None, residual=None, act=LACACHE_ACT
     M, K = a.shape
     N = out.shape[1]
     rows = 2 * N if act == LACACHE_ACT_SWIGLU else N
-    with _on(a, w, out, bias, residual):
-        check(lib().lacache_linear_act_bf16(
-            _stream(stream, a), _ptr(a, _BF16, "a"), _ptr(w, _BF16, "w", (rows, K)),
-            _ptr(bias, _BF16, "bias", (rows,), optional=True),
-            _ptr(residual, _BF16, "residual", (M, N), optional=True), _ptr(out, _BF16, "out", (M, N)), M, N, K, act),
-            "lacache_linear_act_bf16")
+    there = _elsewhere(a, w, out, bias, residual)
+    if there is not None:
+        with there:
+            return lacache_linear_act_bf16(a, w, out, bias, residual, act, stream)
+    check(lib().lacache_linear_act_bf16(
+        _stream(stream, a), _ptr(a, _BF16, "a"), _ptr(w, _BF16, "w", (rows, K)),
+        _ptr(bias, _BF16, "bias", (rows,), optional=True), _ptr(residual, _BF16, "residual", (M, N), optional=True),
+        _ptr(out, _BF16, "out", (M, N)), M, N, K, act), "lacache_linear_act_bf16")
 
 
 def lacache_rope_scatter(qkv, rows, rope_cos, rope_sin, q, k, v, stream=None):
@@ -370,6 +364,11 @@ def lacache_paged_append(qkv, seq_ids, positions, rope_cos, rope_sin, page_table
     page_table [S, max_pages] int32 names. k_cache, v_cache [num_pages, kv_heads, page, d] bf16, or
     e4m3 with k_scale, v_scale [num_pages, kv_heads, page] fp32. rope_cos, rope_sin [rope_len,
     rope_dim / 2] fp32, or None for no rotation."""
+    there = _elsewhere(qkv, seq_ids, positions, rope_cos, rope_sin, page_table, q, k_cache, v_cache, k_scale, v_scale)
+    if there is not None:
+        with there:
+            return lacache_paged_append(qkv, seq_ids, positions, rope_cos, rope_sin, page_table, q, k_cache, v_cache,
+                                        k_scale, v_scale, stream)
     T, heads, d = q.shape
     S, max_pages = page_table.shape
     kc, vc, ks, vs, (num_pages, kv, page, dk), kind = _kv(k_cache, v_cache, k_scale, v_scale)
@@ -382,12 +381,10 @@ def lacache_paged_append(qkv, seq_ids, positions, rope_cos, rope_sin, page_table
         rope_len, half = rope_cos.shape
         rope_dim = 2 * half
         sn = _ptr(rope_sin, _F32, "rope_sin", rope_cos.shape)
-    with _on(qkv, seq_ids, positions, rope_cos, rope_sin, page_table, q, k_cache, v_cache, k_scale, v_scale):
-        check(lib().lacache_paged_append(
-            _stream(stream, qkv), _ptr(qkv, _BF16, "qkv", (T, (heads + 2 * kv) * d)),
-            _ptr(seq_ids, _I32, "seq_ids", (T,)), _ptr(positions, _I32, "positions", (T,)), T, cs, sn, rope_len,
-            rope_dim, _ptr(page_table, _I32, "page_table"), S, max_pages, _ptr(q, _BF16, "q"), kc, vc, ks, vs,
-            num_pages, page, heads, kv, d, kind), "lacache_paged_append")
+    check(lib().lacache_paged_append(
+        _stream(stream, qkv), _ptr(qkv, _BF16, "qkv", (T, (heads + 2 * kv) * d)), _ptr(seq_ids, _I32, "seq_ids", (T,)),
+        _ptr(positions, _I32, "positions", (T,)), T, cs, sn, rope_len, rope_dim, _ptr(page_table, _I32, "page_table"), S,
+        max_pages, _ptr(q, _BF16, "q"), kc, vc, ks, vs, num_pages, page, heads, kv, d, kind), "lacache_paged_append")
 
 
 def lacache_paged_attention(q, k_cache, v_cache, page_table, seq_lens, o, lse=None, k_scale=None, v_scale=None,
@@ -396,21 +393,25 @@ def lacache_paged_attention(q, k_cache, v_cache, page_table, seq_lens, o, lse=No
     (lacache_paged_append), seq_lens [S] int32 keys each; lse [S, nq, heads] fp32 or None. scale is
     1 / sqrt(d) by default. causal: a token sees the keys up to its own place, else all. workspace: a
     uint8 tensor of lacache_paged_attention_workspace_bytes (the library's own without it)."""
+    there = _elsewhere(q, k_cache, v_cache, page_table, seq_lens, o, lse, k_scale, v_scale, workspace)
+    if there is not None:
+        with there:
+            return lacache_paged_attention(q, k_cache, v_cache, page_table, seq_lens, o, lse, k_scale, v_scale, scale,
+                                           causal, workspace, stream)
     S, nq, heads, d = q.shape
     kc, vc, ks, vs, (num_pages, kv, page, dk), kind = _kv(k_cache, v_cache, k_scale, v_scale)
     if dk != d:
         raise ValueError("k_cache: vectors of %d, q of %d" % (dk, d))
     max_pages = page_table.shape[1]
-    with _on(q, k_cache, v_cache, page_table, seq_lens, o, lse, k_scale, v_scale, workspace):
-        args = (_stream(stream, q), _ptr(q, _BF16, "q"), kc, vc, ks, vs,
-                _ptr(page_table, _I32, "page_table", (S, max_pages)), _ptr(seq_lens, _I32, "seq_lens", (S,)),
-                _ptr(o, _BF16, "o", q.shape), _ptr(lse, _F32, "lse", (S, nq, heads), optional=True), S, nq, heads, kv,
-                d, num_pages, page, max_pages, d ** -0.5 if scale is None else scale, int(bool(causal)), kind)
-        if workspace is None:
-            check(lib().lacache_paged_attention(*args), "lacache_paged_attention")
-        else:
-            check(lib().lacache_paged_attention_ws(*args, _ptr(workspace, (torch.uint8,), "workspace"),
-                                                   workspace.numel()), "lacache_paged_attention_ws")
+    args = (_stream(stream, q), _ptr(q, _BF16, "q"), kc, vc, ks, vs,
+            _ptr(page_table, _I32, "page_table", (S, max_pages)), _ptr(seq_lens, _I32, "seq_lens", (S,)),
+            _ptr(o, _BF16, "o", q.shape), _ptr(lse, _F32, "lse", (S, nq, heads), optional=True), S, nq, heads, kv, d,
+            num_pages, page, max_pages, d ** -0.5 if scale is None else scale, int(bool(causal)), kind)
+    if workspace is None:
+        check(lib().lacache_paged_attention(*args), "lacache_paged_attention")
+    else:
+        check(lib().lacache_paged_attention_ws(*args, _ptr(workspace, (torch.uint8,), "workspace"), workspace.numel()),
+              "lacache_paged_attention_ws")
 
 
 def lacache_paged_attention_workspace_bytes(S, nq, heads, kv_heads, d):

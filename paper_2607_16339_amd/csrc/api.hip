@@ -831,7 +831,7 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
 size_t lacache_paged_attention_workspace_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
   if (S < 0 || S > kPagedMaxSeqs || nq <= 0 || nq > kPagedMaxNq || check_heads(heads, kv_heads, d) != LACACHE_OK)
     return 0;
-  return paged_attention_ws_bytes(nq, heads, kv_heads, d);
+  return paged_attention_ws_bytes(S, nq, heads, kv_heads, d);
 }
 
 int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
@@ -845,7 +845,7 @@ int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache
   if (S == 0) return LACACHE_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   void* ws = nullptr;
-  RETURN_IF(get_workspace(st, paged_attention_ws_bytes(nq, heads, kv_heads, d), &ws));
+  RETURN_IF(get_workspace(st, paged_attention_ws_bytes(S, nq, heads, kv_heads, d), &ws));
   return hip_status(launch_paged_attention(st, a, d, cache_type == LACACHE_KV_E4M3, ws));
 }
 
@@ -858,7 +858,7 @@ int lacache_paged_attention_ws(void* stream, const uint16_t* q, const void* k_ca
   RETURN_IF(check_attention(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, o, lse, S, nq, heads, kv_heads,
                             d, num_pages, page, max_pages, scale, causal, cache_type, &a));
   if (S == 0) return LACACHE_OK;
-  const size_t need = paged_attention_ws_bytes(nq, heads, kv_heads, d);
+  const size_t need = paged_attention_ws_bytes(S, nq, heads, kv_heads, d);
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || ws_bytes < need)
     return LACACHE_ERR_INVALID_ARG;
   const size_t rows = static_cast<size_t>(S * nq * heads), places = static_cast<size_t>(num_pages) * kv_heads * page;

@@ -174,11 +174,12 @@ struct PagedAttn {
   int causal;
   float scale_log2;
   // (set by the launcher)
-  float* part;    // the pieces' states
+  int2* cuts;     // [S] pieces of each sequence and the first one's place in part
+  float* part;    // the states of pieces that are joined
   int row_tiles;  // of a KV head's rows
-  int wq;         // pieces aimed at per KV head and row tile
+  int wq;         // pieces per KV head and row tile that fill the chip once
 };
-size_t paged_attention_ws_bytes(int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
+size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws);
 
 }  // namespace lacache

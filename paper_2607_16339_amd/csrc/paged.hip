@@ -90,13 +90,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
 // during softmax and P V, the next values during the next scores, without a
 // barrier. Two workgroups of 4 wavefronts per CU keep 64 to 128 KB in flight.
 //
-// Work is cut on the device, where the lengths are: a sequence of nt tiles gets
-// n = ceil(nt Wq / sum nt) pieces (at most one per 4 tiles, one for an empty one),
-// Wq + S or fewer in all (below 2 Wq of them in sequences of more than one, since
-// n < 2 nt Wq / sum nt there), so that pieces are of about one length whatever the
-// batch; a piece's tiles are divided over the 4 wavefronts, whose states meet in
-// LDS. A sequence of one piece is finished there; those of others are joined by
-// paged_join_kernel, in piece order.
+// Work is cut on the device, where the lengths are: a sequence's tiles into
+// ceil(nt / C) pieces, C (piece_tiles) from all lengths of the call; a piece's tiles
+// are divided over the 4 wavefronts, whose states meet in LDS. A sequence of one
+// piece is finished there; those of others are joined by paged_join_kernel, in
+// piece order. With sum nt <= 2 C Wq there are at most 2 Wq + S pieces, and fewer
+// than 4 Wq in sequences of several (of more than C tiles, so n < 2 nt / C).
 //
 // Softmax in base 2 with the state (m, l, O) in fp32; P enters the second
 // product as two bf16 terms (p = hi + lo, 2^-17 relative: one term would double
@@ -134,7 +133,7 @@ __device__ __forceinline__ int seq_len(const PagedAttn& a, int s) {
   return len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
 }
 
-// Key tiles of all sequences (every lane).
+// Key tiles of all sequences (in every lane).
 template <int kKeys>
 __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
   int n = 0;
@@ -143,14 +142,37 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
   return __builtin_amdgcn_readlane(wave_prefix(n), 63);
 }
 
+// The most tiles of a piece, for all sequences of a call. Wq pieces per KV head and
+// row tile fill the chip once (two workgroups per CU). Pieces of kLong tiles and more
+// (16 per wavefront) hide their start: twice Wq of them, for balance. Shorter ones:
+// the least length at which all pieces run at once, if one below kLong does that.
+constexpr int kLong = 64;
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+template <int kKeys>
+__device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane) {
+  if (a.wq <= 1) return 1 << 30;  // (enough heads: every sequence whole)
+  const int tot = total_tiles<kKeys>(a, lane);
+  const int two = ceil_div(tot, 2 * a.wq);
+  if (two >= kLong) return two;
+  int lo = max(kPagedWaves, ceil_div(tot, a.wq)), hi = kLong;
+  if (a.wq > a.S) hi = min(hi, max(lo, ceil_div(tot, a.wq - a.S)));  // (enough: a piece more per sequence)
+  if (a.S <= 64 && lo < hi) {
+    const int nt = lane < a.S ? ceil_div(seq_len(a, lane), kKeys) : 0;
+    while (lo < hi) {  // (six rounds at most)
+      const int c = (lo + hi) / 2;
+      if (__builtin_amdgcn_readlane(wave_prefix(ceil_div(nt, c)), 63) <= a.wq)
+        hi = c;
+      else
+        lo = c + 1;
+    }
+  }
+  return hi;
+}
+
 // Pieces of a sequence of nt tiles. One of at most kWhole tiles stays whole: four
 // tiles one after the other in each wavefront cost less than a second kernel.
 constexpr int kWhole = 4 * kPagedWaves;
-__device__ __forceinline__ int pieces(int nt, int tot, int wq) {
-  const int n = nt <= kWhole ? 1 : static_cast<int>((static_cast<uint32_t>(nt) * static_cast<uint32_t>(wq) + tot - 1) / tot);
-  const int most = (nt + kPagedWaves - 1) / kPagedWaves;
-  return n < most || n == 1 ? n : most;
-}
+__device__ __forceinline__ int pieces(int nt, int most) { return nt <= kWhole ? 1 : ceil_div(nt, most); }
 
 template <int D, bool kFp8, int RT>
 struct PagedTile {
@@ -225,10 +247,10 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   const int rt = rem >> 3, pair = q8 * 8 + (rem & 7);
   const int h = pair % a.kv_heads;
   int unit = pair / a.kv_heads;
-  const int tot = total_tiles<kKeys>(a, lane);
+  const int most = piece_tiles<kKeys>(a, lane);
   int s = -1, n = 0, slot = 0;  // slot: the place of the sequence's first piece in the workspace
   for (int b = 0; b < a.S; b += 64) {
-    const int mine = b + lane < a.S ? pieces((seq_len(a, b + lane) + kKeys - 1) / kKeys, tot, a.wq) : 0;
+    const int mine = b + lane < a.S ? pieces(ceil_div(seq_len(a, b + lane), kKeys), most) : 0;
     const int upto = wave_prefix(mine), kept = wave_prefix(mine > 1 ? mine : 0);
     const uint64_t behind = __ballot(upto > unit);
     if (behind != 0) {
@@ -243,9 +265,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
     slot += __builtin_amdgcn_readlane(kept, 63);
   }
   if (s < 0) return;  // (fewer pieces than the grid has room for)
+  // what the join needs to know
+  if (unit == 0 && h == 0 && rt == 0 && t == 0) a.cuts[s] = make_int2(n, slot);
   const int len = wave_uniform(seq_len(a, s));
   const int nt = (len + kKeys - 1) / kKeys;
-  // (below 2^32: unit < n <= 4 compute units, nt <= 2^17)
+  // (below 2^32: unit < n <= nt / 4 + 1, nt <= 2^17)
   const int p0 = static_cast<int>(static_cast<uint32_t>(unit) * static_cast<uint32_t>(nt) / n);
   const int p1 = static_cast<int>(static_cast<uint32_t>(unit + 1) * static_cast<uint32_t>(nt) / n);
   const int i0 = p0 + wave * (p1 - p0) / kPagedWaves, i1 = p0 + (wave + 1) * (p1 - p0) / kPagedWaves;
@@ -596,29 +620,22 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
 // piece, in order) joined through LDS in order. Each thread has kAhead pieces'
 // loads in flight, and a long sequence's pieces are spread over up to 32 shares:
 // one thread per 4 dims walking 128 pieces took 95 us (one row of 131072 keys).
-template <int D, int kKeys, int RT>
+template <int D, int RT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
   constexpr int kRows = 16 * RT, kPart = kRows * (D + 2), kAhead = 4;
   __shared__ __align__(16) float so[32][8][4];
   __shared__ float sm[32], sl[32];
-  const int t = threadIdx.x, lane = t & 63;
+  const int t = threadIdx.x;
   const int hrs = a.kv_heads * a.row_tiles;
   const int hr = blockIdx.x % hrs, s = blockIdx.x / hrs;
-  const int tot = total_tiles<kKeys>(a, lane);
-  const int n = pieces((seq_len(a, s) + kKeys - 1) / kKeys, tot, a.wq);
+  const int2 cut = a.cuts[s];
+  const int n = cut.x;
   if (n == 1) return;
-  int before = 0;
-  for (int b = 0; b < s; b += 64)
-    if (b + lane < s) {
-      const int k = pieces((seq_len(a, b + lane) + kKeys - 1) / kKeys, tot, a.wq);
-      before += k > 1 ? k : 0;
-    }
-  before = __builtin_amdgcn_readlane(wave_prefix(before), 63);
   const int h = hr / a.row_tiles, rt = hr - h * a.row_tiles;
   const int left = a.nq * (a.heads / a.kv_heads) - kRows * rt, rows = left < kRows ? left : kRows;
   const int rows2 = rows <= 1 ? 1 : 1 << (32 - __builtin_clz(rows - 1)), pg = 32 / rows2;
   const int64_t stride = static_cast<int64_t>(hrs) * kPart;
-  const float* part = a.part + before * stride + static_cast<int64_t>(hr) * kPart;
+  const float* part = a.part + cut.y * stride + static_cast<int64_t>(hr) * kPart;
   const int c = t & 7, u = t >> 3, row = u & (rows2 - 1), share = u / rows2, c4 = 8 * blockIdx.y + c;
   float m = -kInf, l = 0.0f;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -683,8 +700,8 @@ PagedPlan paged_plan(int64_t nq, int64_t heads, int64_t kv_heads) {
   PagedPlan p;
   p.row_tiles = (R + rows - 1) / rows;
   const int64_t hr = kv_heads * p.row_tiles;
-  p.wq = (4 * device_cu_count() + hr - 1) / hr;
-  p.parts = p.wq == 1 ? 0 : 2 * p.wq * hr;
+  p.wq = (2 * device_cu_count() + hr - 1) / hr;
+  p.parts = p.wq == 1 ? 0 : 4 * p.wq * hr;
   return p;
 }
 
@@ -705,18 +722,21 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
   return hipGetLastError();
 }
 
-size_t paged_attention_ws_bytes(int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
+// The workspace: [S] (pieces, first kept piece), then the kept pieces' states.
+static size_t cuts_bytes(int64_t S) { return (static_cast<size_t>(S) * 8 + 255) / 256 * 256; }
+size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
   const PagedPlan p = paged_plan(nq, heads, kv_heads);
-  const size_t bytes = 256 + static_cast<size_t>(p.parts) * 16 * paged_rt(nq * (heads / kv_heads)) * (d + 2) * 4;
+  const size_t bytes = cuts_bytes(S) + static_cast<size_t>(p.parts) * 16 * paged_rt(nq * (heads / kv_heads)) * (d + 2) * 4;
   return (bytes + 255) / 256 * 256;
 }
 
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws) {
   const PagedPlan p = paged_plan(a.nq, a.heads, a.kv_heads);
-  a.part = static_cast<float*>(ws);
+  a.cuts = static_cast<int2*>(ws);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(a.S));
   a.row_tiles = static_cast<int>(p.row_tiles);
   a.wq = static_cast<int>(p.wq);
-  const int64_t pairs = (p.wq + a.S) * a.kv_heads;
+  const int64_t pairs = ((p.wq == 1 ? 0 : 2 * p.wq) + a.S) * a.kv_heads;
   const dim3 grid(static_cast<unsigned>((pairs + 7) / 8 * 8 * p.row_tiles)), block(64 * kPagedWaves);
   const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles), static_cast<unsigned>(d / 32));
   // (no sequence of several pieces: nothing to join)
@@ -725,7 +745,7 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     constexpr int keys = PagedTile<D_, F_, RT_>::kKeys;                                                     \
     hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                       \
     if (p.wq > 1 && a.max_len > kWhole * keys)                                                              \
-      hipLaunchKernelGGL((paged_join_kernel<D_, keys, RT_>), jgrid, dim3(256), 0, st, a);                   \
+      hipLaunchKernelGGL((paged_join_kernel<D_, RT_>), jgrid, dim3(256), 0, st, a);                   \
   } while (0)
 #define PR(D_, F_)                                                 \
   do {                                                             \
