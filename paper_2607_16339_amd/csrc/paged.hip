@@ -1,5 +1,7 @@
 // Paged key/value cache: rotation and append of new tokens, and their
 // attention over the cache.
+#include <algorithm>
+
 #include "device.h"
 #include "launch.h"
 
@@ -128,17 +130,18 @@ __device__ __forceinline__ int wave_prefix(int x) {
   return x;
 }
 
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
 __device__ __forceinline__ int seq_len(const PagedAttn& a, int s) {
   const int len = a.seq_lens[s];
   return len < 0 ? 0 : (len > a.max_len ? a.max_len : len);
 }
 
-// Key tiles of all sequences (in every lane).
+// Key tiles of all sequences (in every lane); first: those of sequence `lane`.
 template <int kKeys>
-__device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
-  int n = 0;
-  for (int b = 0; b < a.S; b += 64)
-    if (b + lane < a.S) n += (seq_len(a, b + lane) + kKeys - 1) / kKeys;
+__device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane, int first) {
+  int n = first;
+  for (int s = 64 + lane; s < a.S; s += 64) n += ceil_div(seq_len(a, s), kKeys);
   return __builtin_amdgcn_readlane(wave_prefix(n), 63);
 }
 
@@ -147,20 +150,18 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane) {
 // (16 per wavefront) hide their start: twice Wq of them, for balance. Shorter ones:
 // the least length at which all pieces run at once, if one below kLong does that.
 constexpr int kLong = 64;
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 template <int kKeys>
-__device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane) {
+__device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int first) {
   if (a.wq <= 1) return 1 << 30;  // (enough heads: every sequence whole)
-  const int tot = total_tiles<kKeys>(a, lane);
+  const int tot = total_tiles<kKeys>(a, lane, first);
   const int two = ceil_div(tot, 2 * a.wq);
   if (two >= kLong) return two;
   int lo = max(kPagedWaves, ceil_div(tot, a.wq)), hi = kLong;
   if (a.wq > a.S) hi = min(hi, max(lo, ceil_div(tot, a.wq - a.S)));  // (enough: a piece more per sequence)
   if (a.S <= 64 && lo < hi) {
-    const int nt = lane < a.S ? ceil_div(seq_len(a, lane), kKeys) : 0;
     while (lo < hi) {  // (six rounds at most)
       const int c = (lo + hi) / 2;
-      if (__builtin_amdgcn_readlane(wave_prefix(ceil_div(nt, c)), 63) <= a.wq)
+      if (__builtin_amdgcn_readlane(wave_prefix(ceil_div(first, c)), 63) <= a.wq)
         hi = c;
       else
         lo = c + 1;
@@ -247,16 +248,21 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   const int rt = rem >> 3, pair = q8 * 8 + (rem & 7);
   const int h = pair % a.kv_heads;
   int unit = pair / a.kv_heads;
-  const int most = piece_tiles<kKeys>(a, lane);
+  // (the lengths of the first 64 sequences are loaded once: a short call is a chain of loads)
+  const int len0 = lane < a.S ? seq_len(a, lane) : 0;
+  const int most = piece_tiles<kKeys>(a, lane, ceil_div(len0, kKeys));
+  int len = 0;
   int s = -1, n = 0, slot = 0;  // slot: the place of the sequence's first piece in the workspace
   for (int b = 0; b < a.S; b += 64) {
-    const int mine = b + lane < a.S ? pieces(ceil_div(seq_len(a, b + lane), kKeys), most) : 0;
+    const int lenb = b == 0 ? len0 : (b + lane < a.S ? seq_len(a, b + lane) : 0);
+    const int mine = b + lane < a.S ? pieces(ceil_div(lenb, kKeys), most) : 0;
     const int upto = wave_prefix(mine), kept = wave_prefix(mine > 1 ? mine : 0);
     const uint64_t behind = __ballot(upto > unit);
     if (behind != 0) {
       const int at = __builtin_ctzll(behind);
       s = b + at;
       n = __builtin_amdgcn_readlane(mine, at);
+      len = __builtin_amdgcn_readlane(lenb, at);
       unit -= __builtin_amdgcn_readlane(upto, at) - n;
       slot += __builtin_amdgcn_readlane(kept, at) - n;
       break;
@@ -267,7 +273,6 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   if (s < 0) return;  // (fewer pieces than the grid has room for)
   // what the join needs to know
   if (unit == 0 && h == 0 && rt == 0 && t == 0) a.cuts[s] = make_int2(n, slot);
-  const int len = wave_uniform(seq_len(a, s));
   const int nt = (len + kKeys - 1) / kKeys;
   // (below 2^32: unit < n <= nt / 4 + 1, nt <= 2^17)
   const int p0 = static_cast<int>(static_cast<uint32_t>(unit) * static_cast<uint32_t>(nt) / n);
@@ -736,13 +741,19 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(a.S));
   a.row_tiles = static_cast<int>(p.row_tiles);
   a.wq = static_cast<int>(p.wq);
-  const int64_t pairs = ((p.wq == 1 ? 0 : 2 * p.wq) + a.S) * a.kv_heads;
-  const dim3 grid(static_cast<unsigned>((pairs + 7) / 8 * 8 * p.row_tiles)), block(64 * kPagedWaves);
+  // pieces: as many as the lengths may ask for, and as the table's pages can hold
+  auto most_pieces = [&](int keys) {
+    const int64_t nt = (a.max_len + keys - 1) / keys;
+    const int64_t by_len = nt <= kWhole || p.wq == 1 ? 1 : (nt + kPagedWaves - 1) / kPagedWaves;
+    return std::min(2 * p.wq + a.S, a.S * by_len);
+  };
+  const dim3 block(64 * kPagedWaves);
   const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles), static_cast<unsigned>(d / 32));
   // (no sequence of several pieces: nothing to join)
 #define PA(D_, F_, RT_)                                                                                     \
   do {                                                                                                      \
     constexpr int keys = PagedTile<D_, F_, RT_>::kKeys;                                                     \
+    const dim3 grid(static_cast<unsigned>((most_pieces(keys) * a.kv_heads + 7) / 8 * 8 * p.row_tiles));     \
     hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                       \
     if (p.wq > 1 && a.max_len > kWhole * keys)                                                              \
       hipLaunchKernelGGL((paged_join_kernel<D_, RT_>), jgrid, dim3(256), 0, st, a);                   \
