@@ -436,8 +436,9 @@ size_t lacache_first_layer_workspace_bytes(int64_t R, int64_t heads, int64_t H);
  *                                                  in place), else disjoint
  *   out      [M x N] bf16                          (output)
  * out = RNE_bf16(act(a w^T + bias) + residual), all in fp32 with one rounding at
- * the end; the sum is that of lacache_linear_bf16 bit for bit up to 128 rows, and
- * one chain over K above (a row's result does not depend on M on either side):
+ * the end. The sum is either that of lacache_linear_bf16, bit for bit (calls of up
+ * to 128 rows that are bound by reading w), or one chain over K, as the sizes
+ * decide: a row's last bits may differ between calls of different M.
  *   NONE x; RELU max(x, 0); SILU x / (1 + e^-x); GELU x (1 + erf(x / sqrt 2)) / 2
  *   (off by at most 0.75e-7 |x| before the rounding); GELU_TANH x (1 +
  *   tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;

@@ -118,7 +118,7 @@ hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* 
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
 // The tile of the call above: activation rows and weight rows of a workgroup.
 void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]);
-// The same for the few rows (linear_streams_rows) of the weight-streaming kernel.
+// The same on the weight-streaming kernel, for the few rows it takes.
 struct ActArgs;
 bool linear_streams_rows(int64_t M);
 hipError_t launch_linear_act_rows(hipStream_t st, const uint16_t* a, const uint16_t* w, const ActArgs& act, uint16_t* out,

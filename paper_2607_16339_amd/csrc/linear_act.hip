@@ -1,16 +1,18 @@
-// The bf16 projection with its epilogue for many rows: out = act(a W^T + bias) +
-// residual, or silu(gate) up of two products (kGlu: weight rows n and Nw/2 + n,
-// which a wavefront holds as slabs of 16 gate rows and the same 16 up rows).
-// (Up to 128 rows the weight-streaming kernel of the first layer runs with the
-// same epilogue.)
+// The bf16 projection with its epilogue: out = act(a W^T + bias) + residual, or
+// silu(gate) up of two products (kGlu: weight rows n and Nw/2 + n, which a wavefront
+// holds as slabs of 16 gate rows and the same 16 up rows). Calls of few rows that are
+// one stream of weights go to the first layer's kernel, which has the same epilogue.
 //
-// Each output is one chain of 16x16x32 bf16 MFMAs over K in order, whatever the
-// tile, so a row's result does not depend on M among these calls.
+// Each output is one chain of 16x16x32 bf16 MFMAs over K in order, the same bits
+// whatever the tile.
 //
 // K-steps of 64 elements (128 bytes of a row) come by direct copies into an LDS
 // ring, [rows][128 B] with the 16-byte chunk c of row r at c ^ ((r / 2) mod 8):
 // the 16 rows of an operand read touch every bank once. Rows past M and columns
 // past the weight's rows fetch the last one and are not stored.
+#include <algorithm>
+#include <cmath>
+
 #include "activation.h"
 #include "device.h"
 #include "launch.h"
@@ -346,37 +348,49 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
   }
 }
 
-// The tiles, and a call's time on each: rounds of one workgroup per CU of a start and
-// end and K/64 steps, and a step's time that grows with the work in flight. Fitted at
-// 152 sizes, M = 129..8192, N x K = 128 x 4096 to 24576 x 4096 and 16384 x 512, all
-// tiles in turn in one process: on average 0.24 % slower than the best tile, 8 % at
-// most (N = 16384, K = 512). At N = K = 4096, in us on 64 x 64, 64 x 128, 128 x 128,
-// 128 x 256 and 256 x 256: M = 200 17, 23, 32, 52, 88; 512 32, 25, 33, 53, 89; 1024
-// 60, 46, 37, 54, 91; 2048 125, 94, 73, 60, 97; 8192 511, 385, 293, 246, 206.
-// More wavefronts of less work each were better throughout: a step of a lone workgroup
-// is a chain of barrier, LDS reads and products (128 x 128 on 4, 8 and 16 wavefronts,
-// M = 512, N = K = 4096: 43, 36, 33).
+// The tiles, and what a call costs on each: rounds (of `fit` workgroups per CU) of a
+// start and K/64 steps, a step's part in the traffic of the whole chip, and a part
+// for every workgroup that shares a CU. Up to 128 rows the weight-streaming kernel of
+// the first layer (K over four wavefronts, 16 or 48 weight rows) competes. Weighed on
+// 245 sizes with weights from HBM, M = 1..8192, N x K = 128 x 4096 to 24576 x 4096, all
+// kernels in turn in one process: the choice is on average 0.2 % slower than the best,
+// 15 % at most. In us on the streaming kernel, 32 x 64, 64 x 64, 64 x 128, 128 x 128, 128
+// x 256 and 256 x 256:
+//   N = K = 4096       M = 32  11, 17, 19, 27, 30, 67, 80;  128  24, 17, 21, 29, 38, 75, 84
+//   N = 12288, K = 4096     48  36, 30, 25, 34, 35, 71, 83;  128  68, 43, 41, 35, 44, 82, 85
+//   N = 16384, K = 1024     32  17, 8.5, 9.1, 11, 12, 21, 27
+// and of warm weights, N = K = 4096, from 64 x 128 on: M = 512 25, 33, 53, 89; 1024 46, 37,
+// 54, 91; 2048 94, 73, 60, 97; 8192 385, 293, 246, 206. More wavefronts of less work
+// each were better throughout, a step of a lone workgroup being a chain of barrier,
+// LDS reads and products (128 x 128 on 4, 8 and 16 wavefronts, M = 512: 43, 36, 33);
+// 256 x 256 on 4 wavefronts of 128 x 128 took 288 us where these take 218, on 16 of
+// 64 x 64 the same, with 32x32x16 MFMAs 231.
 struct Shape {
-  int bm, bn;
-  double start, c0, c1;
+  int bm, bn, fit;
+  double start, step, chip, shared;
 };
-constexpr Shape kShapes[5] = {{64, 64, 1.75, 0.130, 0.057},
-                              {64, 128, 1.87, 0.208, 0.097},
-                              {128, 128, 1.93, 0.304, 0.176},
-                              {128, 256, 2.28, 0.599, 0.315},
-                              {256, 256, 9.00, 1.032, 0.358}};
+constexpr Shape kShapes[6] = {{32, 64, 2, 0.336, 0.100, 0.071, 0.071},  {64, 64, 2, 0.640, 0.055, 0.136, 0.144},
+                              {64, 128, 1, 0.219, 0.307, 0.137, 0.0},   {128, 128, 1, 1.162, 0.422, 0.182, 0.0},
+                              {128, 256, 1, 0.000, 1.007, 0.226, 0.0},  {256, 256, 1, 5.869, 1.078, 0.624, 0.0}};
+constexpr int kStream = -1;
 
 int best_shape(int64_t M, int64_t Nw, int64_t K) {
-  const int64_t cus = device_cu_count();
-  const double ks = static_cast<double>(K) / 64.0;
-  int pick = 0;
-  double best = 0.0;
-  for (int t = 0; t < 5; ++t) {
+  const double cus = static_cast<double>(device_cu_count()), ks = static_cast<double>(K) / 64.0;
+  int pick = kStream;
+  double best = HUGE_VAL;
+  if (linear_streams_rows(M)) {
+    int tile[2];
+    linear_tile(M, Nw, K, tile);
+    const double items = static_cast<double>(Nw / tile[1] * ((M + 63) / 64));
+    const double kb = static_cast<double>(2 * std::min<int64_t>(4, (M + 15) / 16) + tile[1] / 8);  // of a wavefront's step
+    best = 2.353 + std::ceil(items / cus) * ks / 4 * (0.163 + 0.006 * kb) + 0.031 * ks * items * kb / (4 * cus);
+  }
+  for (int t = 0; t < 6; ++t) {
     const Shape& s = kShapes[t];
-    const int64_t items = ((M + s.bm - 1) / s.bm) * ((Nw + s.bn - 1) / s.bn);
-    const double rounds = static_cast<double>((items + cus - 1) / cus);
-    const double us = rounds * (s.start + s.c0 * ks) + s.c1 * ks * static_cast<double>(items) / static_cast<double>(cus);
-    if (t == 0 || us < best) pick = t, best = us;
+    const double items = static_cast<double>(((M + s.bm - 1) / s.bm) * ((Nw + s.bn - 1) / s.bn));
+    const double per_cu = std::ceil(items / cus);
+    const double cost = std::ceil(per_cu / s.fit) * (s.start + s.step * ks) + s.chip * ks * items / cus + s.shared * ks * per_cu;
+    if (cost < best) pick = t, best = cost;
   }
   return pick;
 }
@@ -393,10 +407,11 @@ hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
                        dim3(64 * WR_ * WC_), 0, st, c);                                                                  \
     break
   switch (shape) {
-    LT(0, 4, 2, 8);
-    LT(1, 2, 4, 6);
-    LT(2, 4, 4, 5);
-    LT(3, 4, 4, 3);
+    LT(0, 2, 2, 6);
+    LT(1, 4, 2, 5);
+    LT(2, 2, 4, 6);
+    LT(3, 4, 4, 5);
+    LT(4, 4, 4, 3);
     default: hipLaunchKernelGGL((linear_act_256_kernel<kGlu>), round, dim3(512), 0, st, c);
   }
 #undef LT
@@ -407,19 +422,19 @@ hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
 
 hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {
-  const ActArgs aa{bias, residual, act};
-  if (linear_streams_rows(M)) return launch_linear_act_rows(st, a, w, aa, out, M, N, K);
   const bool glu = act == LACACHE_ACT_SWIGLU;
-  LinCall c{a, w, out, aa, M, K, glu ? 2 * N : N, 0, 0};
+  const ActArgs aa{bias, residual, act};
+  const LinCall c{a, w, out, aa, M, K, glu ? 2 * N : N, 0, 0};
   const int shape = best_shape(M, c.Nw, K);
+  if (shape == kStream) return launch_linear_act_rows(st, a, w, aa, out, M, N, K);
   return glu ? launch_shape<true>(st, c, shape) : launch_shape<false>(st, c, shape);
 }
 
 void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]) {
   const int64_t Nw = act == LACACHE_ACT_SWIGLU ? 2 * N : N;
-  if (linear_streams_rows(M)) return linear_tile(M, Nw, K, tile);
-  const Shape& s = kShapes[best_shape(M, Nw, K)];
-  tile[0] = s.bm, tile[1] = s.bn;
+  const int shape = best_shape(M, Nw, K);
+  if (shape == kStream) return linear_tile(M, Nw, K, tile);
+  tile[0] = kShapes[shape].bm, tile[1] = kShapes[shape].bn;
 }
 
 }  // namespace lacache

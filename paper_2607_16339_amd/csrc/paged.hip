@@ -8,14 +8,28 @@
 namespace lacache {
 namespace {
 
-// Rotation and append. A group of D/8 lanes holds one head's vector of one
-// token, 8 dims per lane; lane c of the rotated part meets its partner (c +- r/16)
-// by loading that chunk as well (its line is in the cache already).
+// Rotation and append. A group of D/8 lanes holds one head's vector of one token, 8
+// dims per lane; in the rotated part lane c meets its partner c +- r/16 by shuffles.
+// A workgroup takes a token's heads, kBatch vectors of each group in flight at a
+// time (the cosines of the token's position are loaded once for all of them).
 template <int D, bool kFp8>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
-  constexpr int L = D / 8, G = 256 / L;
-  const int c = threadIdx.x % L;
+  constexpr int L = D / 8, G = 256 / L, kBatch = 3;
+  const int lane = threadIdx.x & 63, c = threadIdx.x % L;
   const int64_t t = blockIdx.x;
+  const int HT = a.heads + 2 * a.kv_heads;
+  const uint4* src = reinterpret_cast<const uint4*>(a.qkv + t * HT * D) + c;
+  const int first = blockIdx.y * G + threadIdx.x / L, step = gridDim.y * G;
+  uint4 x[kBatch];
+  auto load = [&](int hs0) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int hs = hs0 + b * step;
+      x[b] = make_uint4(0u, 0u, 0u, 0u);
+      if (hs < HT) x[b] = src[static_cast<int64_t>(hs) * L];
+    }
+  };
+  load(first);
   const int seq = a.seq_ids[t], pos = a.positions[t];
   if (seq < 0 || seq >= a.S || pos < 0 || pos >= a.max_pos) return;
   const int page = a.table[static_cast<int64_t>(seq) * a.max_pages + (pos >> a.page_log2)];
@@ -23,58 +37,65 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
   const int slot = pos & ((1 << a.page_log2) - 1);
   const int hc = a.rope_dim >> 4;  // chunks of half the rotated part
   const bool rot = c < 2 * hc, low = c < hc;
+  const int partner = rot ? (low ? lane + hc : lane - hc) : lane;
   float cs[8], sn[8];
   if (rot) {
     const int64_t o = static_cast<int64_t>(pos) * (8 * hc) + 8 * (low ? c : c - hc);
     const v4f* pc = reinterpret_cast<const v4f*>(a.cs + o);
     const v4f* ps = reinterpret_cast<const v4f*>(a.sn + o);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) cs[e] = pc[e >> 2][e & 3], sn[e] = ps[e >> 2][e & 3];
+    for (int e = 0; e < 8; ++e) {
+      cs[e] = pc[e >> 2][e & 3];
+      sn[e] = low ? -ps[e >> 2][e & 3] : ps[e >> 2][e & 3];  // (x - y and x + (-y) are the same bits)
+    }
   }
-  const int HT = a.heads + 2 * a.kv_heads;
-  const uint4* src = reinterpret_cast<const uint4*>(a.qkv + t * HT * D);
-  for (int hs = blockIdx.y * G + threadIdx.x / L; hs < HT; hs += gridDim.y * G) {
-    const uint4 x = src[hs * L + c];
-    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-    float y[8];
+  for (int hs0 = first; hs0 < HT; hs0 += kBatch * step) {
+    if (hs0 != first) load(hs0);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[2 * e] = bf16lo(xw[e]), y[2 * e + 1] = bf16hi(xw[e]);
-    const bool turn = rot && hs < a.heads + a.kv_heads;
-    if (turn) {
-      const uint4 p = src[hs * L + (low ? c + hc : c - hc)];
-      const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
+    for (int b = 0; b < kBatch; ++b) {
+      const int hs = hs0 + b * step;
+      const uint32_t xw[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
+      uint32_t pw[4];  // (every lane of the wavefront shuffles)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float o = e & 1 ? bf16hi(pw[e >> 1]) : bf16lo(pw[e >> 1]);
-        const float u = y[e] * cs[e], w = o * sn[e];
-        y[e] = low ? u - w : u + w;
+      for (int e = 0; e < 4; ++e) pw[e] = static_cast<uint32_t>(__shfl(static_cast<int>(xw[e]), partner, 64));
+      if (hs >= HT) continue;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[2 * e] = bf16lo(xw[e]), y[2 * e + 1] = bf16hi(xw[e]);
+      const bool turn = rot && hs < a.heads + a.kv_heads;
+      if (turn) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float o = e & 1 ? bf16hi(pw[e >> 1]) : bf16lo(pw[e >> 1]);
+          y[e] = y[e] * cs[e] + o * sn[e];
+        }
       }
-    }
-    const bool to_cache = hs >= a.heads;
-    const bool is_v = hs >= a.heads + a.kv_heads;
-    const int h = is_v ? hs - a.heads - a.kv_heads : hs - a.heads;
-    const int64_t row = ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + slot;
-    if (kFp8 && to_cache) {
-      // the largest magnitude by its bits, so that infinities and NaNs win
-      uint32_t top = 0u;
+      const bool to_cache = hs >= a.heads, is_v = hs >= a.heads + a.kv_heads;
+      const int h = is_v ? hs - a.heads - a.kv_heads : hs - a.heads;
+      const int64_t row = ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + slot;
+      if (kFp8 && to_cache) {
+        // the largest magnitude by its bits, so that infinities and NaNs win
+        uint32_t top = 0u;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7FFFFFFFu);
 #pragma unroll
-      for (int o = L / 2; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, 64)));
-      const float s = __uint_as_float(top) / kE4M3Max;
-      uint32_t lo = 0x7F7F7F7Fu, hi = 0x7F7F7F7Fu;  // a vector that is not finite reads as NaN
-      if (top < 0x7F800000u) quant8(y, s, lo, hi);
-      reinterpret_cast<uint2*>(is_v ? a.v_cache : a.k_cache)[row * L + c] = make_uint2(lo, hi);
-      if (c == 0) (is_v ? a.v_scale : a.k_scale)[row] = s;
-      continue;
+        for (int o = L / 2; o >= 1; o >>= 1)
+          top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, 64)));
+        const float s = __uint_as_float(top) / kE4M3Max;
+        uint32_t lo = 0x7F7F7F7Fu, hi = 0x7F7F7F7Fu;  // a vector that is not finite reads as NaN
+        if (top < 0x7F800000u) quant8(y, s, lo, hi);
+        reinterpret_cast<uint2*>(is_v ? a.v_cache : a.k_cache)[row * L + c] = make_uint2(lo, hi);
+        if (c == 0) (is_v ? a.v_scale : a.k_scale)[row] = s;
+        continue;
+      }
+      const uint4 o = turn ? make_uint4(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]), cvt_pk_bf16(y[4], y[5]),
+                                        cvt_pk_bf16(y[6], y[7]))
+                           : x[b];
+      if (to_cache)
+        reinterpret_cast<uint4*>(is_v ? a.v_cache : a.k_cache)[row * L + c] = o;
+      else
+        reinterpret_cast<uint4*>(a.q)[(t * a.heads + hs) * L + c] = o;
     }
-    const uint4 o = turn ? make_uint4(cvt_pk_bf16(y[0], y[1]), cvt_pk_bf16(y[2], y[3]), cvt_pk_bf16(y[4], y[5]),
-                                      cvt_pk_bf16(y[6], y[7]))
-                         : x;
-    if (to_cache)
-      reinterpret_cast<uint4*>(is_v ? a.v_cache : a.k_cache)[row * L + c] = o;
-    else
-      reinterpret_cast<uint4*>(a.q)[(t * a.heads + hs) * L + c] = o;
   }
 }
 
@@ -156,8 +177,9 @@ __device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int fir
   const int tot = total_tiles<kKeys>(a, lane, first);
   const int two = ceil_div(tot, 2 * a.wq);
   if (two >= kLong) return two;
+  if (a.wq <= a.S) return kLong;  // (as many sequences as fill the chip)
   int lo = max(kPagedWaves, ceil_div(tot, a.wq)), hi = kLong;
-  if (a.wq > a.S) hi = min(hi, max(lo, ceil_div(tot, a.wq - a.S)));  // (enough: a piece more per sequence)
+  hi = min(hi, max(lo, ceil_div(tot, a.wq - a.S)));  // (enough: a piece more per sequence)
   if (a.S <= 64 && lo < hi) {
     while (lo < hi) {  // (six rounds at most)
       const int c = (lo + hi) / 2;
@@ -716,9 +738,8 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
   const int G = static_cast<int>(256 / (d / 8));
   const int HT = a.heads + 2 * a.kv_heads;
   const int per = (HT + G - 1) / G;
-  const int64_t cus = device_cu_count();
-  // few tokens: every head of a token at once
-  const int64_t ny = T * per <= 8 * cus ? per : 1;
+  // few tokens: a workgroup for every G heads of a token else for kBatch times as many
+  const int64_t ny = T * per <= 2 * device_cu_count() ? per : (per + 2) / 3;
   const dim3 grid(static_cast<unsigned>(T), static_cast<unsigned>(ny)), block(256);
   if (d == 128 && fp8) hipLaunchKernelGGL((paged_append_kernel<128, true>), grid, block, 0, st, a);
   else if (d == 128) hipLaunchKernelGGL((paged_append_kernel<128, false>), grid, block, 0, st, a);
@@ -744,8 +765,8 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   // pieces: as many as the lengths may ask for, and as the table's pages can hold
   auto most_pieces = [&](int keys) {
     const int64_t nt = (a.max_len + keys - 1) / keys;
-    const int64_t by_len = nt <= kWhole || p.wq == 1 ? 1 : (nt + kPagedWaves - 1) / kPagedWaves;
-    return std::min(2 * p.wq + a.S, a.S * by_len);
+    if (p.wq == 1 || nt <= (p.wq <= a.S ? kLong : kWhole)) return static_cast<int64_t>(a.S);
+    return std::min(2 * p.wq + a.S, a.S * ((nt + kPagedWaves - 1) / kPagedWaves));
   };
   const dim3 block(64 * kPagedWaves);
   const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles), static_cast<unsigned>(d / 32));
@@ -755,7 +776,7 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     constexpr int keys = PagedTile<D_, F_, RT_>::kKeys;                                                     \
     const dim3 grid(static_cast<unsigned>((most_pieces(keys) * a.kv_heads + 7) / 8 * 8 * p.row_tiles));     \
     hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                       \
-    if (p.wq > 1 && a.max_len > kWhole * keys)                                                              \
+    if (most_pieces(keys) > a.S)                                                                            \
       hipLaunchKernelGGL((paged_join_kernel<D_, RT_>), jgrid, dim3(256), 0, st, a);                   \
   } while (0)
 #define PR(D_, F_)                                                 \

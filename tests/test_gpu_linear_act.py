@@ -1,11 +1,9 @@
 """The bf16 product with bias, activation and residual, on the GPU.
 
-Up to 128 rows the sum before the epilogue is lacache_linear_bf16's (its fp32
-tap, tested elsewhere against 64 bits), so the epilogue is checked in 64 bits on
-that very sum; above, on the sum in 64 bits, off by the fp32 chain's K u sum|a w|
-(u = 2^-24). Tolerance: the output's rounding 2^-8 |ref|, and before it the fp32 steps:
-x = sum + bias (u relative to |x|, which with the sum's error an activation of slope
-at most 1.13 passes on), the activation's hardware exp2 and reciprocal with the
+Against 64 bits. Tolerance: the output's rounding 2^-8 |ref|, and before it the
+fp32 steps: the sum of K exact products in any order, K u sum|a w| (u = 2^-24); x =
+sum + bias (u relative to |x|, which with the sum's error an activation of slope at
+most 1.13 passes on), the activation's hardware exp2 and reciprocal with the
 rounding of its argument (|x| u + 8 u relative for SiLU's and tanh-GELU's
 exponential, whose cube adds 3 u |argument|), erf's formula (0.75e-7 |x|), SwiGLU's product
 and the residual's addition (u each)."""
@@ -50,16 +48,10 @@ def _case(M, N, K, act, bias, residual, seed=0, std=1.0):
 
 
 def _want(a, w, b, r, act):
-    M, rows = a.shape[0], w.shape[0]
-    if M <= 128:
-        tap = torch.empty((M, rows), dtype=torch.float32, device=DEV)
-        lc.lacache_linear_bf16(a, w, torch.empty((M, rows), dtype=torch.bfloat16, device=DEV), tap)
-        x = tap.double()
-        off = torch.zeros_like(x)
-    else:
-        wt = w.double().t().contiguous()
-        x = a.double() @ wt
-        off = a.shape[1] * U * (a.double().abs() @ wt.abs())
+    rows = w.shape[0]
+    wt = w.double().t().contiguous()
+    x = a.double() @ wt
+    off = a.shape[1] * U * (a.double().abs() @ wt.abs())
     if b is not None:
         x = x + b.double()
     if act == SWIGLU:
@@ -127,10 +119,11 @@ def test_residual_updated_in_place(M, act):
     assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
-# (M, N, K) of each tile; ragged rows, and columns where the tile is wider than what is left
-TILES = {(64, 64): [(130, 128, 256), (700, 1152, 640)], (64, 128): [(300, 4224, 512), (1500, 1152, 640)],
-         (128, 128): [(1000, 4096, 256), (1300, 2944, 512)], (128, 256): [(2047, 4096, 384), (2040, 3968, 1024)],
-         (256, 256): [(8000, 4096, 1024), (6000, 2176, 2048)]}
+# (M, N, K) of each tile and of the streaming kernel; ragged rows, and columns where the tile is wider than what is left
+TILES = {(64, 16): [(7, 1024, 4096), (100, 1024, 4096)], (64, 48): [(20, 12288, 4096)],
+         (32, 64): [(60, 1152, 640), (96, 4096, 2048)], (64, 64): [(90, 6144, 2048), (50, 12288, 512)],
+         (64, 128): [(300, 4224, 512), (1500, 1024, 1024)], (128, 128): [(1000, 4096, 256), (1300, 2944, 512)],
+         (128, 256): [(2047, 4096, 384), (2040, 3968, 1024)], (256, 256): [(8000, 4096, 1024), (6000, 2176, 2048)]}
 
 
 @pytest.mark.parametrize("tile", sorted(TILES))
@@ -159,10 +152,11 @@ def test_rows_do_not_depend_on_the_call(act):
 
 
 @pytest.mark.parametrize("M", [1, 16, 33, 64, 100, 128])
-def test_no_epilogue_is_the_plain_product_bit_for_bit(M):
-    a, w, _, _ = _case(M, 1152, 512, NONE, False, False, seed=M)
+def test_streamed_product_is_the_plain_one_bit_for_bit(M):
+    assert lc.lacache_linear_act_tile(M, 1024, 4096)[1] in (16, 48)
+    a, w, _, _ = _case(M, 1024, 4096, NONE, False, False, seed=M)
     a[0, 3] = float("nan")
-    out, plain = (torch.empty((M, 1152), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    out, plain = (torch.empty((M, 1024), dtype=torch.bfloat16, device=DEV) for _ in range(2))
     lc.lacache_linear_act_bf16(a, w, out)
     lc.lacache_linear_bf16(a, w, plain)
     torch.cuda.synchronize()
