@@ -167,20 +167,27 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane, int fir
 }
 
 // The most tiles of a piece, for all sequences of a call. Wq pieces per KV head and
-// row tile fill the chip once (two workgroups per CU). Pieces of kLong tiles and more
-// (16 per wavefront) hide their start: twice Wq of them, for balance. Shorter ones:
-// the least length at which all pieces run at once, if one below kLong does that.
-constexpr int kLong = 64;
-template <int kKeys>
+// row tile fill the chip once. Pieces of kLong tiles and more hide their start:
+// twice Wq of them, for balance. Shorter ones: the least length, from kLeast, at
+// which all pieces run at once, if one below kLong does that. A sequence of at most
+// kWhole tiles stays whole: a second kernel costs more than its few steps.
+// kWays: wavefronts that share a piece's keys. Where they share its rows instead, a
+// piece's state is 64 or 128 rows, four to eight tiles' worth of bytes.
+template <int kWays>
+struct PieceRule {
+  static constexpr int kLeast = kWays == 4 ? 4 : 8, kWhole = kWays == 4 ? 16 : 12, kLong = 64;
+};
+template <int kKeys, int kWays>
 __device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int first) {
+  using P = PieceRule<kWays>;
   if (a.wq <= 1) return 1 << 30;  // (enough heads: every sequence whole)
   const int tot = total_tiles<kKeys>(a, lane, first);
   const int two = ceil_div(tot, 2 * a.wq);
-  if (two >= kLong) return two;
-  if (a.wq <= a.S) return kLong;  // (as many sequences as fill the chip)
-  int lo = max(kPagedWaves, ceil_div(tot, a.wq)), hi = kLong;
+  if (two >= P::kLong) return two;
+  if (a.wq <= a.S) return P::kLong;  // (as many sequences as fill the chip)
+  int lo = max(P::kLeast, ceil_div(tot, a.wq)), hi = P::kLong;
   hi = min(hi, max(lo, ceil_div(tot, a.wq - a.S)));  // (enough: a piece more per sequence)
-  if (a.S <= 64 && lo < hi) {
+  if (a.S <= 64) {
     while (lo < hi) {  // (six rounds at most)
       const int c = (lo + hi) / 2;
       if (__builtin_amdgcn_readlane(wave_prefix(ceil_div(first, c)), 63) <= a.wq)
@@ -192,10 +199,53 @@ __device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int fir
   return hi;
 }
 
-// Pieces of a sequence of nt tiles. One of at most kWhole tiles stays whole: four
-// tiles one after the other in each wavefront cost less than a second kernel.
-constexpr int kWhole = 4 * kPagedWaves;
-__device__ __forceinline__ int pieces(int nt, int most) { return nt <= kWhole ? 1 : ceil_div(nt, most); }
+// Pieces of a sequence of nt tiles.
+template <int kWays>
+__device__ __forceinline__ int pieces(int nt, int most) {
+  return nt <= PieceRule<kWays>::kWhole ? 1 : ceil_div(nt, most);
+}
+
+// A workgroup's piece: tiles p0 .. p1 - 1 of sequence s (of n pieces, the first of
+// which is kept at `slot` where n > 1), KV head h, row tile rt.
+struct Piece {
+  int s, n, unit, slot, len, p0, p1, h, rt;
+};
+template <int kKeys, int kWays>
+__device__ __forceinline__ bool find_piece(const PagedAttn& a, int lane, Piece& p) {
+  // row tiles of one (piece, KV head) together on an XCD
+  const int rt_n = a.row_tiles, per = 8 * rt_n;
+  const int q8 = blockIdx.x / per, rem = blockIdx.x - q8 * per, pair = q8 * 8 + (rem & 7);
+  p.rt = rem >> 3;
+  p.h = pair % a.kv_heads;
+  int unit = pair / a.kv_heads, slot = 0;
+  // (the lengths of the first 64 sequences are loaded once: a short call is a chain of loads)
+  const int len0 = lane < a.S ? seq_len(a, lane) : 0;
+  const int most = piece_tiles<kKeys, kWays>(a, lane, ceil_div(len0, kKeys));
+  for (int b = 0; b < a.S; b += 64) {
+    const int lenb = b == 0 ? len0 : (b + lane < a.S ? seq_len(a, b + lane) : 0);
+    const int mine = b + lane < a.S ? pieces<kWays>(ceil_div(lenb, kKeys), most) : 0;
+    const int upto = wave_prefix(mine), kept = wave_prefix(mine > 1 ? mine : 0);
+    const uint64_t behind = __ballot(upto > unit);
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind);
+      p.s = b + at;
+      p.n = __builtin_amdgcn_readlane(mine, at);
+      p.len = __builtin_amdgcn_readlane(lenb, at);
+      p.unit = unit - (__builtin_amdgcn_readlane(upto, at) - p.n);
+      p.slot = slot + __builtin_amdgcn_readlane(kept, at) - p.n;
+      const int nt = ceil_div(p.len, kKeys);
+      // (below 2^32: unit < n <= nt / 4 + 1, nt <= 2^17)
+      p.p0 = static_cast<int>(static_cast<uint32_t>(p.unit) * static_cast<uint32_t>(nt) / p.n);
+      p.p1 = static_cast<int>(static_cast<uint32_t>(p.unit + 1) * static_cast<uint32_t>(nt) / p.n);
+      // what the join needs to know
+      if (p.unit == 0 && p.h == 0 && p.rt == 0 && threadIdx.x == 0) a.cuts[p.s] = make_int2(p.n, p.slot);
+      return true;
+    }
+    unit -= __builtin_amdgcn_readlane(upto, 63);
+    slot += __builtin_amdgcn_readlane(kept, 63);
+  }
+  return false;  // (fewer pieces than the grid has room for)
+}
 
 template <int D, bool kFp8, int RT>
 struct PagedTile {
@@ -212,7 +262,8 @@ struct PagedTile {
 };
 // A key's 16-byte chunk c lies at c ^ swizzle: keys are read 16 at a time, one
 // chunk of each, values (transposed) in 8 or 16 keys by 32 or 16 bytes, and both
-// then touch every bank once. kU: the part that a copy adds, by its number.
+// then touch every bank once. (The swizzle of a sum of key numbers without common
+// bits is the xor of theirs.)
 template <int RB>
 __device__ __forceinline__ int kswz(int key) {
   return RB == 256 ? key & 15 : (RB == 128 ? (key >> 1) & 7 : (key >> 2) & 3);
@@ -253,179 +304,125 @@ __device__ __forceinline__ void store_out(const PagedAttn& a, int64_t row, int D
   if (a.lse != nullptr && c4 == 0) a.lse[row] = (m + __log2f(l)) * 0.69314718055994531f;
 }
 
-template <int D, bool kFp8, int RT>
-__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(PagedAttn a) {
-  using T = PagedTile<D, kFp8, RT>;
-  constexpr int RB = T::RB, kKeys = T::kKeys, kSub = T::kSub, kRows = 16 * RT, kSteps = D / 32, kDims = D / 16;
-  constexpr int kState = kRows * D * 4;  // a wavefront's O at the end
-  constexpr int kSlot = T::kSlot > kState ? T::kSlot : kState;
-  __shared__ __align__(16) uint8_t smem[kPagedWaves * kSlot];
-  __shared__ float sml[2][kPagedWaves][kRows];
-  const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
-  const int g = lane >> 4, r = lane & 15;
+// Keeps the compiler from holding what is derived from v in registers across a loop.
+template <typename V>
+__device__ __forceinline__ V fresh(V v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
-  // the work item: row tiles of one (piece, KV head) together on an XCD
-  const int rt_n = a.row_tiles, per = 8 * rt_n;
-  const int q8 = blockIdx.x / per, rem = blockIdx.x - q8 * per;
-  const int rt = rem >> 3, pair = q8 * 8 + (rem & 7);
-  const int h = pair % a.kv_heads;
-  int unit = pair / a.kv_heads;
-  // (the lengths of the first 64 sequences are loaded once: a short call is a chain of loads)
-  const int len0 = lane < a.S ? seq_len(a, lane) : 0;
-  const int most = piece_tiles<kKeys>(a, lane, ceil_div(len0, kKeys));
-  int len = 0;
-  int s = -1, n = 0, slot = 0;  // slot: the place of the sequence's first piece in the workspace
-  for (int b = 0; b < a.S; b += 64) {
-    const int lenb = b == 0 ? len0 : (b + lane < a.S ? seq_len(a, b + lane) : 0);
-    const int mine = b + lane < a.S ? pieces(ceil_div(lenb, kKeys), most) : 0;
-    const int upto = wave_prefix(mine), kept = wave_prefix(mine > 1 ? mine : 0);
-    const uint64_t behind = __ballot(upto > unit);
-    if (behind != 0) {
-      const int at = __builtin_ctzll(behind);
-      s = b + at;
-      n = __builtin_amdgcn_readlane(mine, at);
-      len = __builtin_amdgcn_readlane(lenb, at);
-      unit -= __builtin_amdgcn_readlane(upto, at) - n;
-      slot += __builtin_amdgcn_readlane(kept, at) - n;
-      break;
-    }
-    unit -= __builtin_amdgcn_readlane(upto, 63);
-    slot += __builtin_amdgcn_readlane(kept, 63);
+// A wavefront's way to the pages of a sequence: lane x holds the page of keys
+// 16 (sb + x) ..; -1: not to be read.
+template <int D, bool kFp8>
+struct PagedCopy {
+  static constexpr int RB = D * (kFp8 ? 1 : 2), CPR = RB / 16, KPI = 1024 / RB, UPS = 16 / KPI;
+  const int32_t* table;
+  int sb, pages, len, h, lane;
+  uint32_t koff, voff;
+
+  __device__ __forceinline__ void init(const PagedAttn& a, const Piece& p, int lane_) {
+    lane = lane_, len = p.len, h = p.h;
+    table = a.table + static_cast<int64_t>(p.s) * a.max_pages;
+    const int key = lane / CPR, ch = lane % CPR;
+    koff = key * RB + ((ch ^ kswz<RB>(key)) << 4);
+    voff = key * RB + ((ch ^ vswz<RB, kFp8>(key)) << 4);
   }
-  if (s < 0) return;  // (fewer pieces than the grid has room for)
-  // what the join needs to know
-  if (unit == 0 && h == 0 && rt == 0 && t == 0) a.cuts[s] = make_int2(n, slot);
-  const int nt = (len + kKeys - 1) / kKeys;
-  // (below 2^32: unit < n <= nt / 4 + 1, nt <= 2^17)
-  const int p0 = static_cast<int>(static_cast<uint32_t>(unit) * static_cast<uint32_t>(nt) / n);
-  const int p1 = static_cast<int>(static_cast<uint32_t>(unit + 1) * static_cast<uint32_t>(nt) / n);
-  const int i0 = p0 + wave * (p1 - p0) / kPagedWaves, i1 = p0 + (wave + 1) * (p1 - p0) / kPagedWaves;
-
-  // Q^T operands: row kRows rt + 16 x + r, the dims that the K operand's lanes read together
-  const int G = a.heads / a.kv_heads, R = a.nq * G;
-  bf8 qf[RT][kSteps];
-  int limit[RT];  // keys that this lane's row sees
-#pragma unroll
-  for (int x = 0; x < RT; ++x) {
-    const int rr = kRows * rt + 16 * x + r;
-    limit[x] = a.causal ? len - a.nq + rr / G + 1 : len;
-    const uint16_t* src = a.q + out_row(a, s, h, rr < R ? rr : 0) * D;
-#pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) {
-      const int dim = kFp8 ? 64 * (ks >> 1) + 16 * g + 8 * (ks & 1) : 32 * ks + 8 * g;
-      qf[x][ks] = *reinterpret_cast<const bf8*>(src + dim);
-    }
-  }
-  const int shared_end = a.causal ? len - a.nq + 1 : len;  // keys that every row sees
-
-  float m[RT], l[RT];
-  v4f ot[RT][kDims];
-#pragma unroll
-  for (int x = 0; x < RT; ++x) {
-    m[x] = -kInf, l[x] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < kDims; ++d) ot[x][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-
-  uint8_t* const Kt = smem + wave * kSlot;
-  uint8_t* const Vt = Kt + T::kBytes;
-  const float* const Ks = reinterpret_cast<const float*>(Vt + T::kBytes);
-  const float* const Vs = Ks + 64;
-  const uint32_t lds = lds_u32(Kt);
-
-  // pages: lane x holds that of keys 16 (sb + x) ..; -1: not to be read
-  int sb = 0, pages = -1;
-  const int32_t* table = a.table + static_cast<int64_t>(s) * a.max_pages;
-  auto load_pages = [&](int first) {
+  __device__ __forceinline__ void load_pages(const PagedAttn& a, int first) {
     sb = first;
     const int key = (first + lane) * 16;
     const int page = table[(key < a.max_len ? key : a.max_len - 1) >> a.page_log2];
     pages = key < len && page < static_cast<int>(a.num_pages) ? page : -1;
     // (known to the compiler, which would else wait for every copy at each use)
     wait_vm<0>();
-  };
-  // the row of the caches of keys 16 (sb + x) .., or -1
-  auto row_of = [&](int sub) -> int64_t {
+  }
+  // Keys of 16 sub .. + 15 that exist (a prefix), by the pages from 16 sb_ on.
+  __device__ __forceinline__ int count(int pages_, int sb_, int sub) const {
+    const int left = len - 16 * sub;
+    return __builtin_amdgcn_readlane(pages_, sub - sb_) < 0 ? 0 : (left > 16 ? 16 : (left < 0 ? 0 : left));
+  }
+  // Copies those 16 keys (or values) to lds; odd: the tile's second 16, fourth, ...
+  __device__ __forceinline__ void copy16(const PagedAttn& a, bool values, int sub, bool odd, uint32_t lds) const {
     const int page = __builtin_amdgcn_readlane(pages, sub - sb);
     const int in = (sub * 16) & ((1 << a.page_log2) - 1);
-    const int64_t row = page < 0 ? -1 : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
+    // (16 keys of no page: any that exist; they are not used)
+    const int64_t row = page < 0 ? 0 : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
     // (the same in every lane, and the copies take it from scalar registers)
-    return static_cast<int64_t>(static_cast<uint32_t>(wave_uniform(static_cast<int>(row)))) |
-           (static_cast<int64_t>(wave_uniform(static_cast<int>(row >> 32))) << 32);
-  };
-  const int ckey = lane / T::CPR, cch = lane % T::CPR;
-  const uint32_t koff = ckey * RB + ((cch ^ kswz<RB>(ckey)) << 4);
-  const uint32_t voff = ckey * RB + ((cch ^ vswz<RB, kFp8>(ckey)) << 4);
-  // (fresh: keeps the compiler from holding what is derived from it in registers across the loop)
-  auto fresh = [](auto v) {
-    asm volatile("" : "+v"(v));
-    return v;
-  };
-  auto issue = [&](int i, bool values) {
-    const uint32_t off = fresh(values ? voff : koff);
-    const uint8_t* cache = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache);
-    const uint32_t dst = lds + (values ? T::kBytes : 0);
+    const int64_t urow = static_cast<int64_t>(static_cast<uint32_t>(wave_uniform(static_cast<int>(row)))) |
+                         (static_cast<int64_t>(wave_uniform(static_cast<int>(row >> 32))) << 32);
+    const uint8_t* src = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache) + urow * RB;
+    const uint32_t off = fresh(values ? voff : koff) ^
+                         (odd ? static_cast<uint32_t>(values ? vswz<RB, kFp8>(16) : kswz<RB>(16)) << 4 : 0u);
 #pragma unroll
-    for (int tt = 0; tt < kSub; ++tt) {
-      const int64_t row = row_of(i * kSub + tt);
-      // (16 keys of no page: any that exist; they are not used)
-      const uint8_t* src = cache + (row < 0 ? 0 : row) * RB;
-#pragma unroll
-      for (int u = 0; u < T::UPS; ++u) {
-        const int first = 16 * tt + T::KPI * u;
-        const uint32_t x = static_cast<uint32_t>(values ? vswz<RB, kFp8>(first) : kswz<RB>(first)) << 4;
-        dma16s(src + u * 1024, off ^ x, wave_uniform(static_cast<int>(dst + (tt * T::UPS + u) * 1024)));
-      }
+    for (int u = 0; u < UPS; ++u) {
+      const uint32_t x = static_cast<uint32_t>(values ? vswz<RB, kFp8>(KPI * u) : kswz<RB>(KPI * u)) << 4;
+      dma16s(src + u * 1024, off ^ x, wave_uniform(static_cast<int>(lds + u * 1024)));
     }
-    if (kFp8) {
-      // a scale per lane (of a tile of 32 keys twice)
-      const int page = __shfl(pages, i * kSub - sb + (g & (kSub - 1)), 64);
-      const int in = (i * kKeys + (lane & (kKeys - 1))) & ((1 << a.page_log2) - 1);
-      const int64_t row = page < 0 ? r : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
-      dma4((values ? a.v_scale : a.k_scale) + row,
-           wave_uniform(static_cast<int>(lds + 2 * T::kBytes + (values ? 256 : 0))));
-    }
-  };
+  }
+  // The scales of 64 keys from 16 sub on, a lane each; subs: how many 16s there are (of 2: twice).
+  template <int kSubs>
+  __device__ __forceinline__ void copy_scales(const PagedAttn& a, bool values, int sub, uint32_t lds) const {
+    const int page = __shfl(pages, sub - sb + ((lane >> 4) & (kSubs - 1)), 64);
+    const int in = (sub * 16 + (lane & (16 * kSubs - 1))) & ((1 << a.page_log2) - 1);
+    const int64_t row = page < 0 ? lane & 15 : ((static_cast<int64_t>(page) * a.kv_heads + h) << a.page_log2) + in;
+    dma4((values ? a.v_scale : a.k_scale) + row, wave_uniform(static_cast<int>(lds)));
+  }
+};
 
-  // per-lane LDS offsets: K operand chunk 4 step + g of key r; V^T operand (transposing
-  // reads) of keys 4 g .. + 3 and 16 + 4 g .. + 3, dims 16 d ..
-  const int k_base = r * RB + ((g ^ kswz<RB>(r)) << 4);
-  const int vkey = kFp8 ? ((r >> 1) < 4 ? 4 * g + (r >> 1) : 12 + 4 * g + (r >> 1)) : 4 * g + (r >> 2);
-  const int v_base = vkey * RB + (vswz<RB, kFp8>(vkey) << 4) +
-                     (kFp8 ? 8 * (r & 1) : ((((r & 3) >> 1) << 4) | (8 * (r & 1))));
-  auto value_operand = [&](int v_base, int step, int d) -> bf8 {
+// A wavefront's RT tiles of 16 query rows, and what it does with a tile of keys in LDS.
+template <int D, bool kFp8, int RT>
+struct PagedRows {
+  using T = PagedTile<D, kFp8, RT>;
+  static constexpr int RB = T::RB, kKeys = T::kKeys, kSub = T::kSub, kSteps = D / 32, kDims = D / 16;
+  bf8 qf[RT][kSteps];
+  int limit[RT];  // keys that this lane's row sees
+  int seen;       // keys that every row sees
+  float m[RT], l[RT];
+  v4f ot[RT][kDims];  // O~^T: dims 16 d + 4 g .. of row r
+  int lane, g, r, k_base, v_base;
+
+  // Rows row0 .. of KV head h; Q^T with the dims that the K operand's lanes read together.
+  __device__ __forceinline__ void init(const PagedAttn& a, const Piece& p, int row0, int lane_) {
+    lane = lane_, g = lane >> 4, r = lane & 15;
+    const int G = a.heads / a.kv_heads, R = a.nq * G;
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      const int rr = row0 + 16 * x + r;
+      limit[x] = a.causal ? p.len - a.nq + rr / G + 1 : p.len;
+      const uint16_t* src = a.q + out_row(a, p.s, p.h, rr < R ? rr : 0) * D;
+#pragma unroll
+      for (int ks = 0; ks < kSteps; ++ks) {
+        const int dim = kFp8 ? 64 * (ks >> 1) + 16 * g + 8 * (ks & 1) : 32 * ks + 8 * g;
+        qf[x][ks] = *reinterpret_cast<const bf8*>(src + dim);
+      }
+      m[x] = -kInf, l[x] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) ot[x][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    seen = a.causal ? p.len - a.nq + 1 : p.len;
+    // per-lane LDS offsets: K operand chunk 4 step + g of key r; V^T operand (transposing
+    // reads) of keys 4 g .. + 3 and 16 + 4 g .. + 3, dims 16 d ..
+    k_base = r * RB + ((g ^ kswz<RB>(r)) << 4);
+    const int vkey = kFp8 ? ((r >> 1) < 4 ? 4 * g + (r >> 1) : 12 + 4 * g + (r >> 1)) : 4 * g + (r >> 2);
+    v_base = vkey * RB + (vswz<RB, kFp8>(vkey) << 4) +
+             (kFp8 ? 8 * (r & 1) : ((((r & 3) >> 1) << 4) | (8 * (r & 1))));
+  }
+
+  __device__ __forceinline__ bf8 value_operand(const uint8_t* Vt, int vb, int step, int d) const {
     if constexpr (kFp8) {
-      const i2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(Vt + 32 * step * RB + (v_base ^ (d << 4))));
+      const i2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i2*)(Vt + 32 * step * RB + (vb ^ (d << 4))));
       return cvt_fp8x8(static_cast<uint32_t>(w[0]), static_cast<uint32_t>(w[1]));
     } else {
-      const uint8_t* p = Vt + 32 * step * RB + (v_base ^ (d << 5));
+      const uint8_t* p = Vt + 32 * step * RB + (vb ^ (d << 5));
       const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p));
       const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 16 * RB));
       return __builtin_bit_cast(bf8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-  };
-
-  load_pages(i0 * kSub);
-  if (i0 < i1) {
-    issue(i0, false);
-    issue(i0, true);
   }
-  for (int i = i0; i < i1; ++i) {
-    const bool more = i + 1 < i1;
-    // keys of the tile that exist: a prefix of each 16
-    int cnt[kSub];
-    bool whole = true;
-#pragma unroll
-    for (int tt = 0; tt < kSub; ++tt) {
-      const int left = len - (i * kKeys + 16 * tt);
-      cnt[tt] = __builtin_amdgcn_readlane(pages, i * kSub + tt - sb) < 0 ? 0 : (left > 16 ? 16 : (left < 0 ? 0 : left));
-      whole &= cnt[tt] == 16;
-    }
-    const bool differ = (i + 1) * kKeys > shared_end;  // some row does not see all of them
 
-    wait_vm<T::kCopies>();  // the keys have landed
+  // S^T = K Q^T in base 2: sc[x][tt] holds keys 16 tt + 4 g .. of row r. Ks: the keys' scales.
+  __device__ __forceinline__ void scores(const PagedAttn& a, const uint8_t* Kt, const float* Ks,
+                                         v4f (&sc)[RT][kSub]) const {
     const int kb = fresh(k_base);
-    v4f sc[RT][kSub];
 #pragma unroll
     for (int tt = 0; tt < kSub; ++tt) {
 #pragma unroll
@@ -447,34 +444,33 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
         }
       }
     }
-    v4f kscale[kSub];
-    if (kFp8) {
 #pragma unroll
-      for (int tt = 0; tt < kSub; ++tt) kscale[tt] = *reinterpret_cast<const v4f*>(Ks + 16 * tt + 4 * g) * a.scale_log2;
+    for (int tt = 0; tt < kSub; ++tt) {
+      v4f f = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
+      if (kFp8) f = *reinterpret_cast<const v4f*>(Ks + 16 * tt + 4 * g) * a.scale_log2;
+#pragma unroll
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[x][tt][e] *= f[e];
     }
-    wait_lds();
-    if (more) {
-      if ((i + 1) * kSub - sb >= 64) load_pages((i + 1) * kSub);
-      issue(i + 1, false);
-    }
+  }
 
-    // scores in base 2; hidden ones -inf
-#pragma unroll
-    for (int x = 0; x < RT; ++x)
-#pragma unroll
-      for (int tt = 0; tt < kSub; ++tt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[x][tt][e] *= kFp8 ? kscale[tt][e] : a.scale_log2;
-    if (!whole || differ) {
+  // Does no row see key 16 tt + 4 g + e of the tile (from key0 on), or this lane's row not?
+  __device__ __forceinline__ bool hidden(const int (&cnt)[kSub], int key0, int x, int tt, int e) const {
+    return 4 * g + e >= cnt[tt] || key0 + 16 * tt + 4 * g + e >= limit[x];
+  }
+
+  // The online softmax: sc becomes P, the state follows. masked: not every row sees every key.
+  __device__ __forceinline__ void weigh(v4f (&sc)[RT][kSub], const int (&cnt)[kSub], bool masked, int key0) {
+    if (masked) {
 #pragma unroll
       for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int tt = 0; tt < kSub; ++tt)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (4 * g + e >= cnt[tt] || i * kKeys + 16 * tt + 4 * g + e >= limit[x]) sc[x][tt][e] = -kInf;
+            if (hidden(cnt, key0, x, tt, e)) sc[x][tt][e] = -kInf;
     }
-    bf8 ph[RT][kKeys / 32], pl[RT][kKeys / 32];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
       float mx = sc[x][0][0];
@@ -502,11 +498,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
 #pragma unroll
         for (int e = 0; e < 4; ++e) ot[x][d][e] *= alpha;
     }
+  }
 
-    if (more)
-      wait_vm<T::kCopies>();  // the values have landed (the next keys may be in flight)
-    else
-      wait_vm<0>();
+  // O~^T += V^T P^T. whole: every key of the tile exists; differ: some row does not see all of them.
+  __device__ __forceinline__ void values(const PagedAttn& a, uint8_t* Vt, const float* Vs, v4f (&sc)[RT][kSub],
+                                         const int (&cnt)[kSub], bool whole, bool differ, int key0) {
     if (kFp8) {
 #pragma unroll
       for (int tt = 0; tt < kSub; ++tt) {
@@ -517,12 +513,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
           for (int e = 0; e < 4; ++e) {
             const float p = sc[x][tt][e] * vs[e];
             // (a hidden key's scale may be no number)
-            const bool hide = (!whole || differ) &&
-                              (4 * g + e >= cnt[tt] || i * kKeys + 16 * tt + 4 * g + e >= limit[x]);
-            sc[x][tt][e] = hide ? 0.0f : p;
+            sc[x][tt][e] = (!whole || differ) && hidden(cnt, key0, x, tt, e) ? 0.0f : p;
           }
       }
     }
+    bf8 ph[RT][kKeys / 32], pl[RT][kKeys / 32];
 #pragma unroll
     for (int x = 0; x < RT; ++x)
 #pragma unroll
@@ -539,11 +534,11 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
         pl[x][st] = __builtin_bit_cast(bf8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
       }
     if (!whole) {
-      // values of keys that do not exist: zeros
+      // values of keys that do not exist: zeros (every wavefront that reads the tile writes them)
       uint8_t* const mine = Vt + fresh(lane * 16);
 #pragma unroll
       for (int u = 0; u < T::kBytes / 1024; ++u) {
-        const int key = T::KPI * u + ckey;  // (one 16 of the tile per copy)
+        const int key = T::KPI * u + lane / T::CPR;  // (one 16 of the tile per copy)
         if ((key & 15) >= cnt[(T::KPI * u) >> 4]) *reinterpret_cast<uint4*>(mine + u * 1024) = make_uint4(0u, 0u, 0u, 0u);
       }
       asm volatile("" ::: "memory");
@@ -570,7 +565,7 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
       for (int st = 0; st < kKeys / 32; ++st)
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
-          const bf8 vf = value_operand(vb, st, d);
+          const bf8 vf = value_operand(Vt, vb, st, d);
 #pragma unroll
           for (int x = 0; x < RT; ++x) ot[x][d] = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
         }
@@ -580,14 +575,15 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
 #pragma unroll 1
         for (int kk = 0; kk < 32; ++kk) {
           // key kk of the step: element 4 (kk / 16) + kk % 4 of the lanes of group (kk / 4) % 4
-          const int el = 4 * (kk >> 4) + (kk & 3), key = i * kKeys + 32 * st + kk;
+          const int el = 4 * (kk >> 4) + (kk & 3), key = key0 + 32 * st + kk;
           const bool mine = g == ((kk >> 2) & 3);
 #pragma unroll
           for (int d = 0; d < kDims; ++d) {
-            uint4 w = __builtin_bit_cast(uint4, value_operand(vb, st, d));
+            const uint4 w = __builtin_bit_cast(uint4, value_operand(Vt, vb, st, d));
             uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ww[e] = mine && (el >> 1) == e ? (el & 1 ? ww[e] & 0xFFFF0000u : ww[e] & 0xFFFFu) : 0u;
+            for (int e = 0; e < 4; ++e)
+              ww[e] = mine && (el >> 1) == e ? (el & 1 ? ww[e] & 0xFFFF0000u : ww[e] & 0xFFFFu) : 0u;
             const bf8 vf = __builtin_bit_cast(bf8, make_uint4(ww[0], ww[1], ww[2], ww[3]));
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
@@ -598,43 +594,114 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
           }
         }
     }
+  }
+
+  // The lanes that share a row add their parts of l.
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+      l[x] += __shfl_xor(l[x], 16, 64);
+      l[x] += __shfl_xor(l[x], 32, 64);
+    }
+  }
+};
+
+// Up to 32 rows per KV head: the wavefronts of a workgroup share a piece's keys.
+template <int D, bool kFp8, int RT>
+__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(PagedAttn a) {
+  using W = PagedRows<D, kFp8, RT>;
+  using T = typename W::T;
+  constexpr int kKeys = T::kKeys, kSub = T::kSub, kRows = 16 * RT;
+  constexpr int kState = kRows * D * 4;  // a wavefront's O at the end
+  constexpr int kSlot = T::kSlot > kState ? T::kSlot : kState;
+  __shared__ __align__(16) uint8_t smem[kPagedWaves * kSlot];
+  __shared__ float sml[2][kPagedWaves][kRows];
+  const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
+  const int g = lane >> 4, r = lane & 15;
+  Piece p;
+  if (!find_piece<kKeys, kPagedWaves>(a, lane, p)) return;
+  const int i0 = p.p0 + wave * (p.p1 - p.p0) / kPagedWaves, i1 = p.p0 + (wave + 1) * (p.p1 - p.p0) / kPagedWaves;
+  W w;
+  w.init(a, p, kRows * p.rt, lane);
+
+  uint8_t* const Kt = smem + wave * kSlot;
+  uint8_t* const Vt = Kt + T::kBytes;
+  const float* const Ks = reinterpret_cast<const float*>(Vt + T::kBytes);
+  const float* const Vs = Ks + 64;
+  const uint32_t lds = lds_u32(Kt);
+  PagedCopy<D, kFp8> c;
+  c.init(a, p, lane);
+  auto issue = [&](int i, bool values) {
+    const uint32_t dst = lds + (values ? T::kBytes : 0);
+#pragma unroll
+    for (int tt = 0; tt < kSub; ++tt) c.copy16(a, values, i * kSub + tt, tt & 1, dst + tt * 16 * T::RB);
+    if (kFp8) c.template copy_scales<kSub>(a, values, i * kSub, lds + 2 * T::kBytes + (values ? 256 : 0));
+  };
+
+  c.load_pages(a, i0 * kSub);
+  if (i0 < i1) {
+    issue(i0, false);
+    issue(i0, true);
+  }
+  for (int i = i0; i < i1; ++i) {
+    const bool more = i + 1 < i1;
+    int cnt[kSub];
+    bool whole = true;
+#pragma unroll
+    for (int tt = 0; tt < kSub; ++tt) cnt[tt] = c.count(c.pages, c.sb, i * kSub + tt), whole &= cnt[tt] == 16;
+    const bool differ = (i + 1) * kKeys > w.seen;
+    wait_vm<T::kCopies>();  // the keys have landed
+    v4f sc[RT][kSub];
+    w.scores(a, Kt, Ks, sc);
+    wait_lds();
+    if (more) {
+      if ((i + 1) * kSub - c.sb >= 64) c.load_pages(a, (i + 1) * kSub);
+      issue(i + 1, false);
+    }
+    w.weigh(sc, cnt, !whole || differ, i * kKeys);
+    if (more)
+      wait_vm<T::kCopies>();  // the values have landed (the next keys may be in flight)
+    else
+      wait_vm<0>();
+    w.values(a, Vt, Vs, sc, cnt, whole, differ, i * kKeys);
     wait_lds();
     if (more) issue(i + 1, true);
   }
 
   // the wavefronts' states meet: O of row x at 16-byte chunk c ^ row
+  w.finish();
 #pragma unroll
   for (int x = 0; x < RT; ++x) {
-    l[x] += __shfl_xor(l[x], 16, 64);
-    l[x] += __shfl_xor(l[x], 32, 64);
-    if (g == 0) sml[0][wave][16 * x + r] = m[x], sml[1][wave][16 * x + r] = l[x];
+    if (g == 0) sml[0][wave][16 * x + r] = w.m[x], sml[1][wave][16 * x + r] = w.l[x];
 #pragma unroll
-    for (int d = 0; d < kDims; ++d)
-      *reinterpret_cast<v4f*>(Kt + (16 * x + r) * D * 4 + (((4 * d + g) ^ r) << 4)) = ot[x][d];
+    for (int d = 0; d < W::kDims; ++d)
+      *reinterpret_cast<v4f*>(Kt + (16 * x + r) * D * 4 + (((4 * d + g) ^ r) << 4)) = w.ot[x][d];
   }
   __syncthreads();
   constexpr int C4 = D / 4;
-  float* part = a.part + (static_cast<int64_t>(slot + unit) * a.kv_heads * rt_n + h * rt_n + rt) * (kRows * (D + 2));
+  const int R = a.nq * (a.heads / a.kv_heads);
+  float* part = a.part + (static_cast<int64_t>(p.slot + p.unit) * a.kv_heads * a.row_tiles + p.h * a.row_tiles + p.rt) *
+                             (kRows * (D + 2));
 #pragma unroll
   for (int e = t; e < kRows * C4; e += 64 * kPagedWaves) {
-    const int row = e / C4, c4 = e - row * C4, rr = kRows * rt + row;
+    const int row = e / C4, c4 = e - row * C4, rr = kRows * p.rt + row;
     if (rr >= R) continue;
     float mm = -kInf;
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) mm = __builtin_fmaxf(mm, sml[0][w][row]);
+    for (int v = 0; v < kPagedWaves; ++v) mm = __builtin_fmaxf(mm, sml[0][v][row]);
     const float ms = finite_max(mm);
     float ll = 0.0f;
     v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sml[0][w][row] - ms);
-      ll += f * sml[1][w][row];
-      const v4f x = *reinterpret_cast<const v4f*>(smem + w * kSlot + row * D * 4 + ((c4 ^ (row & 15)) << 4));
+    for (int v = 0; v < kPagedWaves; ++v) {
+      const float f = __builtin_amdgcn_exp2f(sml[0][v][row] - ms);
+      ll += f * sml[1][v][row];
+      const v4f x = *reinterpret_cast<const v4f*>(smem + v * kSlot + row * D * 4 + ((c4 ^ (row & 15)) << 4));
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += f * x[k];
     }
-    if (n == 1) {
-      store_out(a, out_row(a, s, h, rr), D, c4, o, mm, ll);
+    if (p.n == 1) {
+      store_out(a, out_row(a, p.s, p.h, rr), D, c4, o, mm, ll);
     } else {
       *reinterpret_cast<v4f*>(part + 2 * kRows + row * D + 4 * c4) = o;
       if (c4 == 0) part[row] = mm, part[kRows + row] = ll;
@@ -642,14 +709,104 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   }
 }
 
-// Joins the pieces of a (sequence, KV head, row tile), 32 dims of them per
+// More rows: RG wavefronts of 32 rows each share every tile of keys, which comes in
+// stages of kTiles tiles (16 or 32 KB) through two LDS buffers, each wavefront
+// copying its share; one barrier per stage. The products and the softmax bound these
+// calls, not the stream: with a row tile of 32 per workgroup, each streaming the keys
+// for itself, 8 sequences x 26 tokens x 16 heads over 2 KV heads (208 rows) took 97 us.
+template <int D, bool kFp8, int RG>
+__global__ __launch_bounds__(64 * RG, 2) void paged_attention_rows_kernel(PagedAttn a) {
+  using W = PagedRows<D, kFp8, 2>;
+  using T = typename W::T;
+  constexpr int kKeys = T::kKeys, kSub = T::kSub, kRows = 32 * RG;
+  constexpr int kTiles = RG * 4096 / T::kBytes, kSubs = kTiles * kSub, kStageKeys = 16 * kSubs;
+  constexpr int kHalf = kTiles * T::kBytes;  // a stage's keys (or values)
+  constexpr int kStage = 2 * kHalf + (kFp8 ? 2 * kStageKeys * 4 : 0);
+  static_assert(kTiles >= 1 && kSubs % RG == 0 && kSubs <= 64 && (!kFp8 || 2 * kStageKeys / 64 % RG == 0), "stage");
+  __shared__ __align__(16) uint8_t smem[2 * kStage];
+  const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
+  Piece p;
+  if (!find_piece<kKeys, 1>(a, lane, p)) return;
+  const int R = a.nq * (a.heads / a.kv_heads), row0 = kRows * p.rt + 32 * wave;
+  W w;
+  w.init(a, p, row0, lane);
+  PagedCopy<D, kFp8> c;
+  c.init(a, p, lane);
+  const uint32_t lds = lds_u32(smem);
+  // this wavefront's share of the stage from tile i on
+  auto issue = [&](int i, int buf) {
+    if ((i + kTiles) * kSub - c.sb > 64) c.load_pages(a, i * kSub);
+    const uint32_t dst = lds + buf * kStage;
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+      for (int b = 0; b < kSubs / RG; ++b) {
+        const int sub = wave + RG * b;
+        c.copy16(a, v != 0, i * kSub + sub, wave & 1, dst + v * kHalf + sub * 16 * T::RB);
+      }
+    if (kFp8) {
+#pragma unroll
+      for (int b = 0; b < 2 * kStageKeys / 64 / RG; ++b) {
+        const int q = wave + RG * b, v = q >= kStageKeys / 64 ? 1 : 0, k = q - v * (kStageKeys / 64);
+        c.template copy_scales<4>(a, v != 0, i * kSub + 4 * k, dst + 2 * kHalf + v * kStageKeys * 4 + k * 256);
+      }
+    }
+  };
+  c.load_pages(a, p.p0 * kSub);
+  if (p.p0 < p.p1) issue(p.p0, 0);
+  for (int i = p.p0, buf = 0; i < p.p1; i += kTiles, buf ^= 1) {
+    const int pages = c.pages, sb = c.sb;  // (the next stage's may be other ones)
+    wait_vm<0>();  // this wavefront's copies of the stage have landed ...
+    bar();         // ... and everyone's; the other buffer has been read
+    if (i + kTiles < p.p1) issue(i + kTiles, buf ^ 1);
+    if (row0 < R) {
+      uint8_t* const K = smem + buf * kStage;
+      const float* const S = reinterpret_cast<const float*>(K + 2 * kHalf);
+#pragma unroll 1
+      for (int q = 0; q < kTiles && i + q < p.p1; ++q) {
+        int cnt[kSub];
+        bool whole = true;
+#pragma unroll
+        for (int tt = 0; tt < kSub; ++tt) cnt[tt] = c.count(pages, sb, (i + q) * kSub + tt), whole &= cnt[tt] == 16;
+        const int key0 = (i + q) * kKeys;
+        const bool differ = key0 + kKeys > w.seen;
+        v4f sc[2][kSub];
+        w.scores(a, K + q * T::kBytes, S + q * kKeys, sc);
+        w.weigh(sc, cnt, !whole || differ, key0);
+        w.values(a, K + kHalf + q * T::kBytes, S + kStageKeys + q * kKeys, sc, cnt, whole, differ, key0);
+      }
+    }
+    wait_lds();
+  }
+  w.finish();
+  float* part = a.part + (static_cast<int64_t>(p.slot + p.unit) * a.kv_heads * a.row_tiles + p.h * a.row_tiles + p.rt) *
+                             (kRows * (D + 2));
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int row = 32 * wave + 16 * x + w.r, rr = kRows * p.rt + row;
+    if (rr >= R) continue;
+    const int64_t dst = out_row(a, p.s, p.h, rr);
+#pragma unroll
+    for (int d = 0; d < W::kDims; ++d) {
+      const int c4 = 4 * d + w.g;
+      if (p.n == 1) {
+        store_out(a, dst, D, c4, w.ot[x][d], w.m[x], w.l[x]);
+      } else {
+        *reinterpret_cast<v4f*>(part + 2 * kRows + row * D + 4 * c4) = w.ot[x][d];
+        if (c4 == 0) part[row] = w.m[x], part[kRows + row] = w.l[x];
+      }
+    }
+  }
+}
+
+// Joins the pieces of a (sequence, KV head, row tile), 32 dims of up to 32 rows per
 // workgroup: 8 threads per (row, share of the pieces), the shares (every pg-th
 // piece, in order) joined through LDS in order. Each thread has kAhead pieces'
 // loads in flight, and a long sequence's pieces are spread over up to 32 shares:
 // one thread per 4 dims walking 128 pieces took 95 us (one row of 131072 keys).
-template <int D, int RT>
+template <int D, int kRows>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
-  constexpr int kRows = 16 * RT, kPart = kRows * (D + 2), kAhead = 4;
+  constexpr int kPart = kRows * (D + 2), kAhead = 4, kSome = kRows < 32 ? kRows : 32;
   __shared__ __align__(16) float so[32][8][4];
   __shared__ float sm[32], sl[32];
   const int t = threadIdx.x;
@@ -659,11 +816,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
   const int n = cut.x;
   if (n == 1) return;
   const int h = hr / a.row_tiles, rt = hr - h * a.row_tiles;
-  const int left = a.nq * (a.heads / a.kv_heads) - kRows * rt, rows = left < kRows ? left : kRows;
+  const int row0 = kSome * (blockIdx.y / (D / 32));
+  const int left = a.nq * (a.heads / a.kv_heads) - kRows * rt - row0, rows = left < kSome ? left : kSome;
+  if (rows <= 0) return;
   const int rows2 = rows <= 1 ? 1 : 1 << (32 - __builtin_clz(rows - 1)), pg = 32 / rows2;
   const int64_t stride = static_cast<int64_t>(hrs) * kPart;
-  const float* part = a.part + cut.y * stride + static_cast<int64_t>(hr) * kPart;
-  const int c = t & 7, u = t >> 3, row = u & (rows2 - 1), share = u / rows2, c4 = 8 * blockIdx.y + c;
+  const float* part = a.part + cut.y * stride + static_cast<int64_t>(hr) * kPart + row0;
+  const int c = t & 7, u = t >> 3, row = u & (rows2 - 1), share = u / rows2;
+  const int c4 = 8 * (blockIdx.y % (D / 32)) + c;
   float m = -kInf, l = 0.0f;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
   if (row < rows) {
@@ -676,7 +836,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
         const float* x = part + (q < n ? q : p) * stride;
         pm[k] = q < n ? x[row] : -kInf;
         pl[k] = x[kRows + row];
-        po[k] = *reinterpret_cast<const v4f*>(x + 2 * kRows + row * D + 4 * c4);
+        po[k] = *reinterpret_cast<const v4f*>(x + 2 * kRows + row0 * (D - 1) + row * D + 4 * c4);  // (x is row0 on)
       }
       float mn = m;
 #pragma unroll
@@ -714,20 +874,24 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += fk * x[e];
   }
-  store_out(a, out_row(a, s, h, kRows * rt + row), D, c4, o, mm, l);
+  store_out(a, out_row(a, s, h, kRows * rt + row0 + row), D, c4, o, mm, l);
 }
 
-// Row tiles of 16 for up to 16 rows per KV head, else of 32.
-int paged_rt(int64_t R) { return R <= 16 ? 1 : 2; }
+// Rows of a workgroup: 16 or 32 where its wavefronts share the keys, 64 or 128 on 2 or
+// 4 wavefronts that share the rows.
 struct PagedPlan {
+  int rows, ways;
   int64_t row_tiles, wq, parts;  // parts: piece states that a call may keep
 };
 PagedPlan paged_plan(int64_t nq, int64_t heads, int64_t kv_heads) {
-  const int64_t R = nq * (heads / kv_heads), rows = 16 * paged_rt(R);
+  const int64_t R = nq * (heads / kv_heads);
   PagedPlan p;
-  p.row_tiles = (R + rows - 1) / rows;
+  p.rows = R <= 16 ? 16 : (R <= 32 ? 32 : (R <= 64 ? 64 : 128));
+  p.ways = R <= 32 ? kPagedWaves : 1;
+  p.row_tiles = (R + p.rows - 1) / p.rows;
   const int64_t hr = kv_heads * p.row_tiles;
-  p.wq = (2 * device_cu_count() + hr - 1) / hr;
+  const int64_t fit = p.rows == 64 ? 4 : 2;  // workgroups per CU (8 wavefronts)
+  p.wq = (fit * device_cu_count() + hr - 1) / hr;
   p.parts = p.wq == 1 ? 0 : 4 * p.wq * hr;
   return p;
 }
@@ -752,7 +916,7 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
 static size_t cuts_bytes(int64_t S) { return (static_cast<size_t>(S) * 8 + 255) / 256 * 256; }
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
   const PagedPlan p = paged_plan(nq, heads, kv_heads);
-  const size_t bytes = cuts_bytes(S) + static_cast<size_t>(p.parts) * 16 * paged_rt(nq * (heads / kv_heads)) * (d + 2) * 4;
+  const size_t bytes = cuts_bytes(S) + static_cast<size_t>(p.parts) * p.rows * (d + 2) * 4;
   return (bytes + 255) / 256 * 256;
 }
 
@@ -764,31 +928,39 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   a.wq = static_cast<int>(p.wq);
   // pieces: as many as the lengths may ask for, and as the table's pages can hold
   auto most_pieces = [&](int keys) {
+    using Keys = PieceRule<kPagedWaves>;
+    using Rows = PieceRule<1>;
     const int64_t nt = (a.max_len + keys - 1) / keys;
-    if (p.wq == 1 || nt <= (p.wq <= a.S ? kLong : kWhole)) return static_cast<int64_t>(a.S);
-    return std::min(2 * p.wq + a.S, a.S * ((nt + kPagedWaves - 1) / kPagedWaves));
+    const int64_t whole = p.wq <= a.S ? Keys::kLong : (p.ways > 1 ? Keys::kWhole : Rows::kWhole);
+    const int64_t least = p.ways > 1 ? Keys::kLeast : Rows::kLeast;
+    if (p.wq == 1 || nt <= whole) return static_cast<int64_t>(a.S);
+    return std::min(2 * p.wq + a.S, a.S * ((nt + least - 1) / least));
   };
-  const dim3 block(64 * kPagedWaves);
-  const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles), static_cast<unsigned>(d / 32));
-  // (no sequence of several pieces: nothing to join)
-#define PA(D_, F_, RT_)                                                                                     \
-  do {                                                                                                      \
-    constexpr int keys = PagedTile<D_, F_, RT_>::kKeys;                                                     \
-    const dim3 grid(static_cast<unsigned>((most_pieces(keys) * a.kv_heads + 7) / 8 * 8 * p.row_tiles));     \
-    hipLaunchKernelGGL((paged_attention_kernel<D_, F_, RT_>), grid, block, 0, st, a);                       \
-    if (most_pieces(keys) > a.S)                                                                            \
-      hipLaunchKernelGGL((paged_join_kernel<D_, RT_>), jgrid, dim3(256), 0, st, a);                   \
-  } while (0)
-#define PR(D_, F_)                                                 \
-  do {                                                             \
-    if (paged_rt(static_cast<int64_t>(a.nq) * (a.heads / a.kv_heads)) == 1) PA(D_, F_, 1); \
-    else PA(D_, F_, 2);                                            \
-  } while (0)
-  if (d == 128 && fp8) PR(128, true);
-  else if (d == 128) PR(128, false);
-  else if (fp8) PR(64, true);
-  else PR(64, false);
-#undef PR
+  auto launch = [&](auto kernel, auto join, int keys, int threads) {
+    const int64_t n = most_pieces(keys);
+    const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
+    if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
+    const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles),
+                     static_cast<unsigned>(d / 32 * (p.rows > 32 ? p.rows / 32 : 1)));
+    hipLaunchKernelGGL(join, jgrid, dim3(256), 0, st, a);
+  };
+#define PA(D_, F_)                                                                                                     \
+  switch (p.rows) {                                                                                                    \
+    case 16: launch(paged_attention_kernel<D_, F_, 1>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys, 256); break;     \
+    case 32: launch(paged_attention_kernel<D_, F_, 2>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys, 256); break;     \
+    case 64: launch(paged_attention_rows_kernel<D_, F_, 2>, paged_join_kernel<D_, 64>, PagedTile<D_, F_, 2>::kKeys, 128); break; \
+    default: launch(paged_attention_rows_kernel<D_, F_, 4>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys, 256);      \
+  }
+  if (d == 128 && fp8) {
+    PA(128, true)
+  } else if (d == 128) {
+    PA(128, false)
+  } else if (fp8) {
+    PA(64, true)
+  } else {
+    PA(64, false)
+  }
 #undef PA
   return hipGetLastError();
 }

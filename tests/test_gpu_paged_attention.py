@@ -59,6 +59,27 @@ def test_long_and_ragged(lens, heads, kv, d, fp8):
     check_attention(c, _q(c, 1), True, what="lens %s.. d %d fp8 %d" % (lens[:3], d, fp8))
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,heads,kv,page,causal,lens", [
+    (9, 8, 2, 16, True, [3000, 40, 0, 700]),      # 36 rows per KV head
+    (16, 4, 1, 64, False, [1500, 16, 33]),        # 64
+    (13, 16, 2, 32, True, [2500, 13, 6]),         # 104
+    (32, 8, 2, 256, False, [1000, 513]),          # 128
+    (26, 16, 2, 16, True, [1900, 1027, 30]),      # 208: two row tiles, the second not full
+    (64, 6, 1, 128, False, [700]),                # 384
+])
+def test_many_rows_over_long_sequences(nq, heads, kv, page, causal, lens, d, fp8):
+    c = Cache(lens, heads, kv, d, page, fp8, seed=nq * heads)
+    check_attention(c, _q(c, nq), causal, what="nq %d heads %d/%d d %d" % (nq, heads, kv, d))
+
+
+def test_many_rows_in_one_long_sequence():
+    # several pages of page numbers, and pieces of several
+    c = Cache([20011], 8, 1, 128, 16, False, seed=77)
+    check_attention(c, _q(c, 12), True, what="96 rows over 20011 keys")
+
+
 def test_many_sequences():
     # more sequences than a wavefront has lanes
     lens = [(37 * i) % 200 for i in range(700)]
@@ -98,7 +119,7 @@ def test_bad_pages_and_lengths(causal, fp8):
 
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
-@pytest.mark.parametrize("nq,heads", [(6, 4), (40, 2)])
+@pytest.mark.parametrize("nq,heads", [(6, 4), (40, 1), (40, 2)])
 def test_hidden_keys_do_not_reach_a_row(bad, nq, heads, fp8):
     """A key or value that is no number changes only the rows that see it, causal rows before it not."""
     c = Cache([100], heads, 1, 128, 16, fp8, seed=13)
