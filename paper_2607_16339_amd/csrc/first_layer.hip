@@ -130,11 +130,13 @@ __device__ __forceinline__ uint16_t* rope_dst(const RopeArgs& ra, int head) {
   return (part == 0 ? ra.q : (part == 1 ? ra.k : ra.v)) + static_cast<int64_t>(head - part * ra.heads) * ra.N * 128;
 }
 
-// What the two projection kernels do with a sum: kPlain rounds and stores it,
-// kRope is above, kAct stores act(sum + bias) + residual and kSwiGlu
-// silu(gate + bias) (up + bias) + residual, where output column n is made of
-// weight rows n (gate) and N + n (up), which meet in one wavefront as a pair of
-// kRope does. The sums before the epilogue are kPlain's, bit for bit.
+// What the projection kernel for a few rows does with a sum: kPlain rounds and
+// stores it, kRope is above (the tiled kernel has these two), kAct stores
+// act(sum + bias) + residual and kSwiGlu silu(gate + bias) (up + bias) + residual,
+// where output column n is made of weight rows n (gate) and N + n (up), which lie
+// in one slab as a pair of kRope does. The sums before the epilogue are kPlain's,
+// bit for bit, and its time is kPlain's too: the weights' stream bounds it (32 rows,
+// N = K = 4096, residual: 8.9 us; gate and up of N = 12288: 38.9 us = 5.2 TB/s).
 constexpr int kPlain = 0, kRope = 1, kAct = 2, kSwiGlu = 3;
 template <int kEpi>
 struct EpiOf {

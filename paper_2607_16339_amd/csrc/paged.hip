@@ -104,11 +104,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
 //
 // The nq heads / kv_heads query rows of a KV head share its keys and values, so
 // they are the columns of one product: S^T = K Q^T, O^T = V^T P^T with 16x16x32
-// bf16 MFMAs, RT tiles of 16 rows. What a call cannot do without is one read of
-// the sequences' keys and values, and every choice serves that stream:
+// bf16 MFMAs, RT tiles of 16 rows. What a call of up to 64 rows per KV head cannot
+// do without is one read of the sequences' keys and values, and every choice serves
+// that stream (for more rows see paged_attention_rows_kernel):
 //
-// A wavefront works alone on a run of key tiles (32 keys of 256 bytes, 64 of
-// fewer) through two LDS slots of its own, one of keys and one of values, each
+// A wavefront works alone on a run of key tiles (of 32 or 64 keys, see PagedTile)
+// through two LDS slots of its own, one of keys and one of values, each
 // refilled by direct copies as soon as it has been read: the next keys fly
 // during softmax and P V, the next values during the next scores, without a
 // barrier. Two workgroups of 4 wavefronts per CU keep 64 to 128 KB in flight.
@@ -130,6 +131,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
 // -inf and value rows of zeros in LDS (0 times a NaN would be one); in the tiles
 // where causal rows differ, values that are not finite send the tile through
 // one product per key, whose result the hiding rows do not take.
+//
+// Measured (32 heads over 8 KV heads, D = 128; a large copy moves 5.05 TB/s): 48
+// sequences of 1..8191 keys, bf16, 157 us = 5.3 TB/s; 64 of 12000..16384, e4m3, 64
+// heads, 368 us = 5.2 TB/s; one of 131072, e4m3, 59 us = 4.7 TB/s; one of 500, 9.4 us
+// with the call's way through the host, the chain of loads length - page - keys -
+// values being what its kernel waits for.
 // ---------------------------------------------------------------------------
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
@@ -172,7 +179,7 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane, int fir
 // which all pieces run at once, if one below kLong does that. A sequence of at most
 // kWhole tiles stays whole: a second kernel costs more than its few steps.
 // kWays: wavefronts that share a piece's keys. Where they share its rows instead, a
-// piece's state is 64 or 128 rows, four to eight tiles' worth of bytes.
+// piece's state is 128 rows, eight tiles' worth of bytes.
 template <int kWays>
 struct PieceRule {
   static constexpr int kLeast = kWays == 4 ? 4 : 8, kWhole = kWays == 4 ? 16 : 12, kLong = 64;
@@ -606,7 +613,7 @@ struct PagedRows {
   }
 };
 
-// Up to 32 rows per KV head: the wavefronts of a workgroup share a piece's keys.
+// Up to 64 rows per KV head, 16 or 32 per workgroup: its wavefronts split a piece's keys.
 template <int D, bool kFp8, int RT>
 __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(PagedAttn a) {
   using W = PagedRows<D, kFp8, RT>;
@@ -709,13 +716,19 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   }
 }
 
-// More rows: RG wavefronts of 32 rows each share every tile of keys, which comes in
-// stages of kTiles tiles (16 or 32 KB) through two LDS buffers, each wavefront
-// copying its share; one barrier per stage. The products and the softmax bound these
-// calls, not the stream: with a row tile of 32 per workgroup, each streaming the keys
-// for itself, 8 sequences x 26 tokens x 16 heads over 2 KV heads (208 rows) took 97 us.
-template <int D, bool kFp8, int RG>
-__global__ __launch_bounds__(64 * RG, 2) void paged_attention_rows_kernel(PagedAttn a) {
+// More than 64 rows: four wavefronts of 32 rows each share every tile of keys, which
+// comes in stages of kTiles tiles (16 KB of keys, 16 of values) through two LDS
+// buffers, each wavefront copying its share; one barrier per stage. The products and
+// the softmax bound these calls, not the stream (208 rows: 215 TFLOP/s). Against row
+// tiles of 32 whose wavefronts split the keys (8 sequences of 1000..4096 keys, 8 KV
+// heads, D = 128): 72 rows 38.2 us against 43.9, 96 39.4 / 44.3, 128 42.5 / 43.6,
+// 256 78.4 / 87.4; 64 sequences of 128 rows and 500..1024 keys 71.6 / 89.6. For up
+// to 64 rows two row tiles of 32 are the better choice: 19.1 us against 21.9 for 8
+// sequences of 1000 keys, 67 / 86 for one of 65536, 96 / 111 for 32 of 1000..4096
+// (two wavefronts of 32 rows instead of four: 22.2, 92 and 86).
+template <int D, bool kFp8>
+__global__ __launch_bounds__(256, 2) void paged_attention_rows_kernel(PagedAttn a) {
+  constexpr int RG = 4;
   using W = PagedRows<D, kFp8, 2>;
   using T = typename W::T;
   constexpr int kKeys = T::kKeys, kSub = T::kSub, kRows = 32 * RG;
@@ -877,8 +890,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
   store_out(a, out_row(a, s, h, kRows * rt + row0 + row), D, c4, o, mm, l);
 }
 
-// Rows of a workgroup: 16 or 32 where its wavefronts share the keys, 64 or 128 on 2 or
-// 4 wavefronts that share the rows.
+// Rows of a workgroup: 16 or 32 where its wavefronts split the keys, 128 where they
+// split the rows (the times of both stand at that kernel).
 struct PagedPlan {
   int rows, ways;
   int64_t row_tiles, wq, parts;  // parts: piece states that a call may keep
@@ -886,12 +899,11 @@ struct PagedPlan {
 PagedPlan paged_plan(int64_t nq, int64_t heads, int64_t kv_heads) {
   const int64_t R = nq * (heads / kv_heads);
   PagedPlan p;
-  p.rows = R <= 16 ? 16 : (R <= 32 ? 32 : (R <= 64 ? 64 : 128));
-  p.ways = R <= 32 ? kPagedWaves : 1;
+  p.rows = R <= 16 ? 16 : (R <= 64 ? 32 : 128);
+  p.ways = R <= 64 ? kPagedWaves : 1;
   p.row_tiles = (R + p.rows - 1) / p.rows;
   const int64_t hr = kv_heads * p.row_tiles;
-  const int64_t fit = p.rows == 64 ? 4 : 2;  // workgroups per CU (8 wavefronts)
-  p.wq = (fit * device_cu_count() + hr - 1) / hr;
+  p.wq = (2 * device_cu_count() + hr - 1) / hr;
   p.parts = p.wq == 1 ? 0 : 4 * p.wq * hr;
   return p;
 }
@@ -902,7 +914,10 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
   const int G = static_cast<int>(256 / (d / 8));
   const int HT = a.heads + 2 * a.kv_heads;
   const int per = (HT + G - 1) / G;
-  // few tokens: a workgroup for every G heads of a token else for kBatch times as many
+  // Few tokens: a workgroup for every G vectors of a token, the chip not being full
+  // otherwise (48 vectors of 128 dims: 16 tokens 3.0 us against 3.3, 64 in e4m3 3.7
+  // against 4.2); from then on one for 3 G, whose loads are in flight together (512
+  // tokens 4.5 us against 4.8).
   const int64_t ny = T * per <= 2 * device_cu_count() ? per : (per + 2) / 3;
   const dim3 grid(static_cast<unsigned>(T), static_cast<unsigned>(ny)), block(256);
   if (d == 128 && fp8) hipLaunchKernelGGL((paged_append_kernel<128, true>), grid, block, 0, st, a);
@@ -936,10 +951,10 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     if (p.wq == 1 || nt <= whole) return static_cast<int64_t>(a.S);
     return std::min(2 * p.wq + a.S, a.S * ((nt + least - 1) / least));
   };
-  auto launch = [&](auto kernel, auto join, int keys, int threads) {
+  auto launch = [&](auto kernel, auto join, int keys) {
     const int64_t n = most_pieces(keys);
     const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
     if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
     const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles),
                      static_cast<unsigned>(d / 32 * (p.rows > 32 ? p.rows / 32 : 1)));
@@ -947,10 +962,9 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   };
 #define PA(D_, F_)                                                                                                     \
   switch (p.rows) {                                                                                                    \
-    case 16: launch(paged_attention_kernel<D_, F_, 1>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys, 256); break;     \
-    case 32: launch(paged_attention_kernel<D_, F_, 2>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys, 256); break;     \
-    case 64: launch(paged_attention_rows_kernel<D_, F_, 2>, paged_join_kernel<D_, 64>, PagedTile<D_, F_, 2>::kKeys, 128); break; \
-    default: launch(paged_attention_rows_kernel<D_, F_, 4>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys, 256);      \
+    case 16: launch(paged_attention_kernel<D_, F_, 1>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys); break; \
+    case 32: launch(paged_attention_kernel<D_, F_, 2>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys); break; \
+    default: launch(paged_attention_rows_kernel<D_, F_>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys);     \
   }
   if (d == 128 && fp8) {
     PA(128, true)
