@@ -112,11 +112,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
 // through two LDS slots of its own, one of keys and one of values, each
 // refilled by direct copies as soon as it has been read: the next keys fly
 // during softmax and P V, the next values during the next scores, without a
-// barrier. Two workgroups of 4 wavefronts per CU keep 64 to 128 KB in flight.
+// barrier. Eight wavefronts per CU, in one workgroup or two (paged_plan), keep 64 to
+// 128 KB in flight.
 //
 // Work is cut on the device, where the lengths are: a sequence's tiles into
 // ceil(nt / C) pieces, C (piece_tiles) from all lengths of the call; a piece's tiles
-// are divided over the 4 wavefronts, whose states meet in LDS. A sequence of one
+// are divided over the wavefronts, whose states meet in LDS. A sequence of one
 // piece is finished there; those of others are joined by paged_join_kernel, in
 // piece order. With sum nt <= 2 C Wq there are at most 2 Wq + S pieces, and fewer
 // than 4 Wq in sequences of several (of more than C tiles, so n < 2 nt / C).
@@ -144,7 +145,6 @@ typedef int i2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s4 lds_s4;
 typedef __attribute__((address_space(3))) i2 lds_i2;
 
-constexpr int kPagedWaves = 4;
 constexpr float kInf = __builtin_inff();
 
 // Sum over lanes 0 .. l of a wavefront.
@@ -178,11 +178,11 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane, int fir
 // twice Wq of them, for balance. Shorter ones: the least length, from kLeast, at
 // which all pieces run at once, if one below kLong does that. A sequence of at most
 // kWhole tiles stays whole: a second kernel costs more than its few steps.
-// kWays: wavefronts that share a piece's keys. Where they share its rows instead, a
-// piece's state is 128 rows, eight tiles' worth of bytes.
+// kWays: wavefronts that split a piece's keys; 1: they split its rows, and a piece's
+// state is 128 rows, eight tiles' worth of bytes.
 template <int kWays>
 struct PieceRule {
-  static constexpr int kLeast = kWays == 4 ? 4 : 8, kWhole = kWays == 4 ? 16 : 12, kLong = 64;
+  static constexpr int kLeast = 8, kWhole = kWays > 1 ? 32 : 12, kLong = 64;
 };
 template <int kKeys, int kWays>
 __device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int first) {
@@ -241,7 +241,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttn& a, int lane, Piece& 
       p.unit = unit - (__builtin_amdgcn_readlane(upto, at) - p.n);
       p.slot = slot + __builtin_amdgcn_readlane(kept, at) - p.n;
       const int nt = ceil_div(p.len, kKeys);
-      // (below 2^32: unit < n <= nt / 4 + 1, nt <= 2^17)
+      // (below 2^32: n <= 2 Wq <= 4 CUs as C >= nt / (2 Wq), and nt <= 2^17)
       p.p0 = static_cast<int>(static_cast<uint32_t>(p.unit) * static_cast<uint32_t>(nt) / p.n);
       p.p1 = static_cast<int>(static_cast<uint32_t>(p.unit + 1) * static_cast<uint32_t>(nt) / p.n);
       // what the join needs to know
@@ -613,21 +613,22 @@ struct PagedRows {
   }
 };
 
-// Up to 64 rows per KV head, 16 or 32 per workgroup: its wavefronts split a piece's keys.
-template <int D, bool kFp8, int RT>
-__global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(PagedAttn a) {
+// Up to 64 rows per KV head, 16 or 32 per workgroup: its kWaves wavefronts split a
+// piece's keys.
+template <int D, bool kFp8, int RT, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAttn a) {
   using W = PagedRows<D, kFp8, RT>;
   using T = typename W::T;
   constexpr int kKeys = T::kKeys, kSub = T::kSub, kRows = 16 * RT;
   constexpr int kState = kRows * D * 4;  // a wavefront's O at the end
   constexpr int kSlot = T::kSlot > kState ? T::kSlot : kState;
-  __shared__ __align__(16) uint8_t smem[kPagedWaves * kSlot];
-  __shared__ float sml[2][kPagedWaves][kRows];
+  __shared__ __align__(16) uint8_t smem[kWaves * kSlot];
+  __shared__ float sml[2][kWaves][kRows];
   const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
   const int g = lane >> 4, r = lane & 15;
   Piece p;
-  if (!find_piece<kKeys, kPagedWaves>(a, lane, p)) return;
-  const int i0 = p.p0 + wave * (p.p1 - p.p0) / kPagedWaves, i1 = p.p0 + (wave + 1) * (p.p1 - p.p0) / kPagedWaves;
+  if (!find_piece<kKeys, kWaves>(a, lane, p)) return;
+  const int i0 = p.p0 + wave * (p.p1 - p.p0) / kWaves, i1 = p.p0 + (wave + 1) * (p.p1 - p.p0) / kWaves;
   W w;
   w.init(a, p, kRows * p.rt, lane);
 
@@ -690,17 +691,17 @@ __global__ __launch_bounds__(64 * kPagedWaves, 2) void paged_attention_kernel(Pa
   float* part = a.part + (static_cast<int64_t>(p.slot + p.unit) * a.kv_heads * a.row_tiles + p.h * a.row_tiles + p.rt) *
                              (kRows * (D + 2));
 #pragma unroll
-  for (int e = t; e < kRows * C4; e += 64 * kPagedWaves) {
+  for (int e = t; e < kRows * C4; e += 64 * kWaves) {
     const int row = e / C4, c4 = e - row * C4, rr = kRows * p.rt + row;
     if (rr >= R) continue;
     float mm = -kInf;
 #pragma unroll
-    for (int v = 0; v < kPagedWaves; ++v) mm = __builtin_fmaxf(mm, sml[0][v][row]);
+    for (int v = 0; v < kWaves; ++v) mm = __builtin_fmaxf(mm, sml[0][v][row]);
     const float ms = finite_max(mm);
     float ll = 0.0f;
     v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int v = 0; v < kPagedWaves; ++v) {
+    for (int v = 0; v < kWaves; ++v) {
       const float f = __builtin_amdgcn_exp2f(sml[0][v][row] - ms);
       ll += f * sml[1][v][row];
       const v4f x = *reinterpret_cast<const v4f*>(smem + v * kSlot + row * D * 4 + ((c4 ^ (row & 15)) << 4));
@@ -892,18 +893,28 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
 
 // Rows of a workgroup: 16 or 32 where its wavefronts split the keys, 128 where they
 // split the rows (the times of both stand at that kernel).
+// Where the wavefronts split the keys: one workgroup of 8 per CU while the sequences,
+// uncut, are too few for two of 4. Shorter runs per wavefront cost less than a cut
+// with its join: 8 blocks of 32 tokens, 700..1024 keys and 32 heads 25.6 us against
+// 30.6, 32 tokens with 200..1024 keys 17.8 / 22.9, 8 with 100..1000 12.2 / 14.4, 48
+// with 1..8191 154.7 / 156.6 (longer sequences that have to be cut are even, 1 to
+// 131072 keys, or lose to their longer pieces, 8 of 1000..4096 23.9 / 22.0). With more
+// sequences two workgroups of 4 per CU hide each other's start and end: 128 of
+// 50..500 keys 31.2 us against 39.0, of 100..2000 in e4m3 66.9 / 77.0 (of 250..2500 in
+// bf16 145 / 138, but their lengths are not known here).
 struct PagedPlan {
   int rows, ways;
   int64_t row_tiles, wq, parts;  // parts: piece states that a call may keep
 };
-PagedPlan paged_plan(int64_t nq, int64_t heads, int64_t kv_heads) {
+PagedPlan paged_plan(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads) {
   const int64_t R = nq * (heads / kv_heads);
   PagedPlan p;
   p.rows = R <= 16 ? 16 : (R <= 64 ? 32 : 128);
-  p.ways = R <= 64 ? kPagedWaves : 1;
   p.row_tiles = (R + p.rows - 1) / p.rows;
   const int64_t hr = kv_heads * p.row_tiles;
   p.wq = (2 * device_cu_count() + hr - 1) / hr;
+  p.ways = R > 64 ? 1 : (S < p.wq ? 8 : 4);
+  if (p.ways == 8) p.wq = (device_cu_count() + hr - 1) / hr;
   p.parts = p.wq == 1 ? 0 : 4 * p.wq * hr;
   return p;
 }
@@ -930,42 +941,48 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
 // The workspace: [S] (pieces, first kept piece), then the kept pieces' states.
 static size_t cuts_bytes(int64_t S) { return (static_cast<size_t>(S) * 8 + 255) / 256 * 256; }
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
-  const PagedPlan p = paged_plan(nq, heads, kv_heads);
+  const PagedPlan p = paged_plan(S, nq, heads, kv_heads);
   const size_t bytes = cuts_bytes(S) + static_cast<size_t>(p.parts) * p.rows * (d + 2) * 4;
   return (bytes + 255) / 256 * 256;
 }
 
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws) {
-  const PagedPlan p = paged_plan(a.nq, a.heads, a.kv_heads);
+  const PagedPlan p = paged_plan(a.S, a.nq, a.heads, a.kv_heads);
   a.cuts = static_cast<int2*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(a.S));
   a.row_tiles = static_cast<int>(p.row_tiles);
   a.wq = static_cast<int>(p.wq);
   // pieces: as many as the lengths may ask for, and as the table's pages can hold
   auto most_pieces = [&](int keys) {
-    using Keys = PieceRule<kPagedWaves>;
+    using Keys = PieceRule<8>;
     using Rows = PieceRule<1>;
     const int64_t nt = (a.max_len + keys - 1) / keys;
     const int64_t whole = p.wq <= a.S ? Keys::kLong : (p.ways > 1 ? Keys::kWhole : Rows::kWhole);
-    const int64_t least = p.ways > 1 ? Keys::kLeast : Rows::kLeast;
+    const int64_t least = Keys::kLeast;
+    static_assert(Keys::kLeast == Rows::kLeast, "one bound for both");
     if (p.wq == 1 || nt <= whole) return static_cast<int64_t>(a.S);
     return std::min(2 * p.wq + a.S, a.S * ((nt + least - 1) / least));
   };
   auto launch = [&](auto kernel, auto join, int keys) {
     const int64_t n = most_pieces(keys);
     const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, grid, dim3(p.ways == 8 ? 512 : 256), 0, st, a);
     if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
     const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles),
                      static_cast<unsigned>(d / 32 * (p.rows > 32 ? p.rows / 32 : 1)));
     hipLaunchKernelGGL(join, jgrid, dim3(256), 0, st, a);
   };
-#define PA(D_, F_)                                                                                                     \
-  switch (p.rows) {                                                                                                    \
-    case 16: launch(paged_attention_kernel<D_, F_, 1>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys); break; \
-    case 32: launch(paged_attention_kernel<D_, F_, 2>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys); break; \
-    default: launch(paged_attention_rows_kernel<D_, F_>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys);     \
-  }
+#define PA(D_, F_)                                                                                              \
+  if (p.rows == 128)                                                                                            \
+    launch(paged_attention_rows_kernel<D_, F_>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys);       \
+  else if (p.rows == 32 && p.ways == 8)                                                                         \
+    launch(paged_attention_kernel<D_, F_, 2, 8>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys);       \
+  else if (p.rows == 32)                                                                                        \
+    launch(paged_attention_kernel<D_, F_, 2, 4>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys);       \
+  else if (p.ways == 8)                                                                                         \
+    launch(paged_attention_kernel<D_, F_, 1, 8>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys);       \
+  else                                                                                                          \
+    launch(paged_attention_kernel<D_, F_, 1, 4>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys);
   if (d == 128 && fp8) {
     PA(128, true)
   } else if (d == 128) {

@@ -87,6 +87,15 @@ def test_many_sequences():
     check_attention(c, _q(c, 1), True, what="700 sequences")
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,heads", [(1, 16), (1, 64), (20, 16), (40, 16)])
+def test_more_sequences_than_the_chip_takes_at_once(nq, heads, d, fp8):
+    # of every length around a border, and one of several pieces
+    c = Cache(EDGES + [5000] + EDGES, heads, 16, d, 32, fp8, seed=heads + nq)
+    check_attention(c, _q(c, nq), True, what="nq %d heads %d d %d fp8 %d" % (nq, heads, d, fp8))
+
+
 @pytest.mark.parametrize("scale", [0.0, 1e-3, 1.0])
 def test_scales_of_the_scores(scale):
     c = Cache([1, 90, 200], 4, 2, 128, 32, False, seed=3)
