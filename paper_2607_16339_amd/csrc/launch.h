@@ -178,6 +178,7 @@ struct PagedAttn {
   float* part;    // the states of pieces that are joined
   int row_tiles;  // of a KV head's rows
   int wq;         // pieces per KV head and row tile that fill the chip once
+  int whole;      // no sequence can have several pieces (the table is too short, or the heads are enough)
 };
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws);

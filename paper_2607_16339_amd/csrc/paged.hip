@@ -225,6 +225,12 @@ __device__ __forceinline__ bool find_piece(const PagedAttn& a, int lane, Piece& 
   p.rt = rem >> 3;
   p.h = pair % a.kv_heads;
   int unit = pair / a.kv_heads, slot = 0;
+  if (a.whole) {
+    if (unit >= a.S) return false;
+    p.s = unit, p.n = 1, p.unit = 0, p.slot = 0;
+    p.len = seq_len(a, unit), p.p0 = 0, p.p1 = ceil_div(p.len, kKeys);
+    return true;
+  }
   // (the lengths of the first 64 sequences are loaded once: a short call is a chain of loads)
   const int len0 = lane < a.S ? seq_len(a, lane) : 0;
   const int most = piece_tiles<kKeys, kWays>(a, lane, ceil_div(len0, kKeys));
@@ -646,7 +652,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
     if (kFp8) c.template copy_scales<kSub>(a, values, i * kSub, lds + 2 * T::kBytes + (values ? 256 : 0));
   };
 
-  c.load_pages(a, i0 * kSub);
+  // (of a short table all of them, without waiting for the length)
+  c.load_pages(a, a.max_len <= 1024 ? 0 : i0 * kSub);
   if (i0 < i1) {
     issue(i0, false);
     issue(i0, true);
@@ -965,6 +972,7 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
   };
   auto launch = [&](auto kernel, auto join, int keys) {
     const int64_t n = most_pieces(keys);
+    a.whole = n == a.S;
     const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
     hipLaunchKernelGGL(kernel, grid, dim3(p.ways == 8 ? 512 : 256), 0, st, a);
     if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
