@@ -155,8 +155,9 @@ struct PagedAppend {
   int64_t max_pages, num_pages;
   int S, max_pos;  // positions below max_pos have a page and a row of the tables
   int heads, kv_heads, rope_dim, page_log2;
+  int groups_log2;  // (set by the launcher) groups of lanes that take a token's vectors
 };
-hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, int64_t d, bool fp8);
+hipError_t launch_paged_append(hipStream_t st, PagedAppend a, int64_t T, int64_t d, bool fp8);
 
 struct PagedAttn {
   const uint16_t* q;  // [S x nq x heads x d]
@@ -178,6 +179,7 @@ struct PagedAttn {
   float* part;    // the states of pieces that are joined
   int row_tiles;  // of a KV head's rows
   int wq;         // pieces per KV head and row tile that fill the chip once
+  int join_rows;  // of a workgroup of the join
   int whole;      // no sequence can have several pieces (the table is too short, or the heads are enough)
 };
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);

@@ -11,15 +11,21 @@ namespace {
 // Rotation and append. A group of D/8 lanes holds one head's vector of one token, 8
 // dims per lane; in the rotated part lane c meets its partner c +- r/16 by shuffles.
 // A workgroup takes a token's heads, kBatch vectors of each group in flight at a
-// time (the cosines of the token's position are loaded once for all of them).
-template <int D, bool kFp8>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
+// time (the cosines of the token's position are loaded once for all of them), or
+// several tokens of few heads (kTokens: T of them in all).
+template <int D, bool kFp8, bool kTokens>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int64_t T) {
   constexpr int L = D / 8, G = 256 / L, kBatch = 3;
-  const int lane = threadIdx.x & 63, c = threadIdx.x % L;
-  const int64_t t = blockIdx.x;
+  const int lane = threadIdx.x & 63, c = threadIdx.x % L, group = threadIdx.x / L;
   const int HT = a.heads + 2 * a.kv_heads;
+  int64_t t = blockIdx.x;
+  int first = blockIdx.y * G + group, step = gridDim.y * G;
+  if (kTokens) {
+    t = (t * G + group) >> a.groups_log2;
+    step = 1 << a.groups_log2, first = group & (step - 1);
+    if (t >= T) return;  // (whole groups, and only lanes of a group shuffle)
+  }
   const uint4* src = reinterpret_cast<const uint4*>(a.qkv + t * HT * D) + c;
-  const int first = blockIdx.y * G + threadIdx.x / L, step = gridDim.y * G;
   uint4 x[kBatch];
   auto load = [&](int hs0) {
 #pragma unroll
@@ -55,7 +61,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a) {
     for (int b = 0; b < kBatch; ++b) {
       const int hs = hs0 + b * step;
       const uint32_t xw[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
-      uint32_t pw[4];  // (every lane of the wavefront shuffles)
+      uint32_t pw[4];  // (every lane of the group shuffles)
 #pragma unroll
       for (int e = 0; e < 4; ++e) pw[e] = static_cast<uint32_t>(__shfl(static_cast<int>(xw[e]), partner, 64));
       if (hs >= HT) continue;
@@ -820,14 +826,15 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows_kernel(PagedAttn 
   }
 }
 
-// Joins the pieces of a (sequence, KV head, row tile), 32 dims of up to 32 rows per
+// Joins the pieces of a (sequence, KV head, row tile), 32 dims of join_rows rows per
 // workgroup: 8 threads per (row, share of the pieces), the shares (every pg-th
 // piece, in order) joined through LDS in order. Each thread has kAhead pieces'
 // loads in flight, and a long sequence's pieces are spread over up to 32 shares:
-// one thread per 4 dims walking 128 pieces took 95 us (one row of 131072 keys).
+// one thread per 4 dims walking 128 pieces took 95 us (one row of 131072 keys); with
+// one share for 28 rows' 256 pieces the call took 65 us, with 8 of them 27.
 template <int D, int kRows>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
-  constexpr int kPart = kRows * (D + 2), kAhead = 4, kSome = kRows < 32 ? kRows : 32;
+  constexpr int kPart = kRows * (D + 2), kAhead = 4;
   __shared__ __align__(16) float so[32][8][4];
   __shared__ float sm[32], sl[32];
   const int t = threadIdx.x;
@@ -837,8 +844,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
   const int n = cut.x;
   if (n == 1) return;
   const int h = hr / a.row_tiles, rt = hr - h * a.row_tiles;
-  const int row0 = kSome * (blockIdx.y / (D / 32));
-  const int left = a.nq * (a.heads / a.kv_heads) - kRows * rt - row0, rows = left < kSome ? left : kSome;
+  const int row0 = a.join_rows * (blockIdx.y / (D / 32));
+  const int left = min(kRows, a.nq * (a.heads / a.kv_heads) - kRows * rt) - row0, rows = min(left, a.join_rows);
   if (rows <= 0) return;
   const int rows2 = rows <= 1 ? 1 : 1 << (32 - __builtin_clz(rows - 1)), pg = 32 / rows2;
   const int64_t stride = static_cast<int64_t>(hrs) * kPart;
@@ -928,7 +935,7 @@ PagedPlan paged_plan(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads) {
 
 }  // namespace
 
-hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, int64_t d, bool fp8) {
+hipError_t launch_paged_append(hipStream_t st, PagedAppend a, int64_t T, int64_t d, bool fp8) {
   const int G = static_cast<int>(256 / (d / 8));
   const int HT = a.heads + 2 * a.kv_heads;
   const int per = (HT + G - 1) / G;
@@ -936,12 +943,29 @@ hipError_t launch_paged_append(hipStream_t st, const PagedAppend& a, int64_t T, 
   // otherwise (48 vectors of 128 dims: 16 tokens 3.0 us against 3.3, 64 in e4m3 3.7
   // against 4.2); from then on one for 3 G, whose loads are in flight together (512
   // tokens 4.5 us against 4.8).
-  const int64_t ny = T * per <= 2 * device_cu_count() ? per : (per + 2) / 3;
-  const dim3 grid(static_cast<unsigned>(T), static_cast<unsigned>(ny)), block(256);
-  if (d == 128 && fp8) hipLaunchKernelGGL((paged_append_kernel<128, true>), grid, block, 0, st, a);
-  else if (d == 128) hipLaunchKernelGGL((paged_append_kernel<128, false>), grid, block, 0, st, a);
-  else if (fp8) hipLaunchKernelGGL((paged_append_kernel<64, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((paged_append_kernel<64, false>), grid, block, 0, st, a);
+  const bool few = T * per <= 2 * device_cu_count();
+  const int ny = few ? per : (per + 2) / 3;
+  // Heads that leave half the groups idle: several tokens per workgroup (6 vectors of 64
+  // dims in e4m3, 97024 tokens: 31 us against 90).
+  const int need = few ? HT : (HT + 2) / 3;
+  a.groups_log2 = 0;
+  while ((1 << a.groups_log2) < need) ++a.groups_log2;
+  const bool tokens = (1 << a.groups_log2) < G;
+  const int64_t at_once = tokens ? G >> a.groups_log2 : 1;
+  const dim3 grid(static_cast<unsigned>((T + at_once - 1) / at_once), static_cast<unsigned>(tokens ? 1 : ny)), block(256);
+#define PP(D_, F_)                                                                                  \
+  if (tokens) hipLaunchKernelGGL((paged_append_kernel<D_, F_, true>), grid, block, 0, st, a, T);    \
+  else hipLaunchKernelGGL((paged_append_kernel<D_, F_, false>), grid, block, 0, st, a, T)
+  if (d == 128 && fp8) {
+    PP(128, true);
+  } else if (d == 128) {
+    PP(128, false);
+  } else if (fp8) {
+    PP(64, true);
+  } else {
+    PP(64, false);
+  }
+#undef PP
   return hipGetLastError();
 }
 
@@ -976,8 +1000,14 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
     hipLaunchKernelGGL(kernel, grid, dim3(p.ways == 8 ? 512 : 256), 0, st, a);
     if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
-    const dim3 jgrid(static_cast<unsigned>(a.S * a.kv_heads * p.row_tiles),
-                     static_cast<unsigned>(d / 32 * (p.rows > 32 ? p.rows / 32 : 1)));
+    // the join: as few rows per workgroup (as many shares of the pieces) as fill the chip
+    const int64_t R = static_cast<int64_t>(a.nq) * (a.heads / a.kv_heads), rows = std::min<int64_t>(R, p.rows);
+    const int64_t joins = static_cast<int64_t>(a.S) * a.kv_heads * p.row_tiles, dims = d / 32;
+    a.join_rows = 4;  // (more shares than 8 take longer to meet than they save)
+    while (a.join_rows < 32 && a.join_rows < rows &&
+           joins * dims * ((rows + a.join_rows - 1) / a.join_rows) > 4 * device_cu_count())
+      a.join_rows *= 2;
+    const dim3 jgrid(static_cast<unsigned>(joins), static_cast<unsigned>(dims * ((rows + a.join_rows - 1) / a.join_rows)));
     hipLaunchKernelGGL(join, jgrid, dim3(256), 0, st, a);
   };
 #define PA(D_, F_)                                                                                              \
