@@ -246,19 +246,20 @@ __global__ __launch_bounds__(64 * WR * WC) void linear_act_tile_kernel(LinCall c
   Epi::store(c, acc, reinterpret_cast<float*>(ring + wave * Epi::kBytes), m0 + 16 * MT * wm, ct, wn, lane);
 }
 
-// 256 x 256 tiles, 8 wavefronts of 64 x 128, walked by at most one workgroup per CU.
-// Two wavefronts share a SIMD and alternate: one reads its operands and issues
+// 256 x 256 or 128 x 256 tiles, 8 wavefronts of 64 x 128 or 64 x 64, walked by at most
+// one workgroup per CU. Two wavefronts share a SIMD and alternate: one reads its operands and issues
 // copies while the other multiplies, a barrier between the phases. Wavefronts 0-3
-// copy the activation rows (ring of 2 steps), 4-7 the weight rows (of 3).
-template <bool kGlu>
-__global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
-  constexpr int BM = 256, BN = 256, MT = 4, NT = 8, kA = BM * 128, kB = BN * 128, DA = 2, DB = 3, P = 8;
+// copy the activation rows (ring of DA steps), 4-7 the weight rows (of DB).
+template <bool kGlu, int BM, int BN, int DA, int DB>
+__global__ __launch_bounds__(512) void linear_act_pairs_kernel(LinCall c) {
+  constexpr int WC = 8 / (BM / 64), MT = 4, NT = BN / WC / 16, kA = BM * 128, kB = BN * 128;
+  constexpr int PA = BM / 32, PB = BN / 32, P = PA > PB ? PA : PB;
   using Epi = Epilogue<kGlu, BN, MT, NT, 2>;
   static_assert(DA * kA + DB * kB <= 163840 && 8 * Epi::kBytes <= DA * kA + DB * kB, "tile shape");
   __shared__ __align__(16) uint8_t ring[DA * kA + DB * kB];
   uint8_t* const sB = ring + DA * kA;
   const int t = threadIdx.x, lane = t & 63, wave = wave_uniform(t >> 6);
-  const int q = lane >> 4, lr = lane & 15, wm = wave >> 1, wn = wave & 1;
+  const int q = lane >> 4, lr = lane & 15, wm = wave / WC, wn = wave % WC;
   const bool late = wave >= 4;  // copies weights, half a phase behind the others
   const int KS = static_cast<int>(c.K / 64);
   const uint32_t K2 = static_cast<uint32_t>(c.K) * 2u;
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
     uint32_t off[P];
 #pragma unroll
     for (int u = 0; u < P; ++u) {
-      const int g = (wave & 3) + 4 * u;
+      const int g = (wave & 3) + 4 * u;  // (up to PA or PB of them are used)
       const uint32_t x = cp.chunk ^ ((g & 1) << 6);
       off[u] = late ? static_cast<uint32_t>(weight_row<kGlu, BN, NT>(c.Nw, ct, 8 * g + cp.crow) -
                                             (kGlu ? 0 : static_cast<int64_t>(ct) * BN)) * K2 + x
@@ -284,34 +285,34 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
       const uint8_t* g = base + static_cast<int64_t>(ks < KS ? ks : KS - 1) * 128;
       const int l = static_cast<int>(lds_u32(dst)) + (wave & 3) * 1024;
 #pragma unroll
-      for (int u = 0; u < P; ++u) dma16s(g, off[u], wave_uniform(l + u * 4096));
+      for (int u = 0; u < P; ++u)
+        if (u < (late ? PB : PA)) dma16s(g, off[u], wave_uniform(l + u * 4096));
     };
     auto landed = [&]() {
       if (late)
-        wait_vm<(DB - 2) * P>();
+        wait_vm<(DB - 2) * PB>();
       else
-        wait_vm<(DA - 2) * P>();
+        wait_vm<(DA - 2) * PA>();
     };
     v4f acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    if (late) {
-      issue(0, sB);
-      issue(1, sB + kB);
-    } else {
-      issue(0, ring);
+#pragma unroll
+    for (int s = 0; s < (DA > DB ? DA : DB) - 1; ++s) {
+      if (late && s < DB - 1) issue(s, sB + s * kB);
+      if (!late && s < DA - 1) issue(s, ring + s * kA);
     }
     landed();
     bar();  // step 0 is in LDS
     if (late) bar();
-    int cur = 0;
+    int ca = 0, cb = 0;
     for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint8_t* pa = ring + (ks & 1) * kA + frag[h] + MT * wm * 2048;
-        const uint8_t* pb = sB + cur * kB + frag[h] + NT * wn * 2048;
+        const uint8_t* pa = ring + ca * kA + frag[h] + MT * wm * 2048;
+        const uint8_t* pb = sB + cb * kB + frag[h] + NT * wn * 2048;
         bf8 af[MT], bf[NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) af[i] = *reinterpret_cast<const bf8*>(pa + i * 2048);
@@ -319,9 +320,9 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
         for (int j = 0; j < NT; ++j) bf[j] = *reinterpret_cast<const bf8*>(pb + j * 2048);
         if (h == 0) {  // into the stages of step ks - 1, which every wavefront has read
           if (late)
-            issue(ks + DB - 1, sB + (cur == 0 ? DB - 1 : cur - 1) * kB);
+            issue(ks + DB - 1, sB + (cb == 0 ? DB - 1 : cb - 1) * kB);
           else
-            issue(ks + DA - 1, ring + ((ks + 1) & 1) * kA);
+            issue(ks + DA - 1, ring + (ca == 0 ? DA - 1 : ca - 1) * kA);
         }
         if (h == 1 && late) landed();
         wait_lds();
@@ -338,7 +339,8 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
         if (h == 1 && !late) landed();
         bar();
       }
-      cur = cur + 1 == DB ? 0 : cur + 1;
+      ca = ca + 1 == DA ? 0 : ca + 1;
+      cb = cb + 1 == DB ? 0 : cb + 1;
     }
     if (!late) bar();
     wait_vm<0>();  // the trailing repeat copies
@@ -352,26 +354,32 @@ __global__ __launch_bounds__(512) void linear_act_256_kernel(LinCall c) {
 // start and K/64 steps, a step's part in the traffic of the whole chip, and a part
 // for every workgroup that shares a CU. Up to 128 rows the weight-streaming kernel of
 // the first layer (K over four wavefronts, 16 or 48 weight rows) competes. Weighed on
-// 245 sizes with weights from HBM, M = 1..8192, N x K = 128 x 4096 to 24576 x 4096, all
-// kernels in turn in one process: the choice is on average 0.2 % slower than the best,
-// 15 % at most. In us on the streaming kernel, 32 x 64, 64 x 64, 64 x 128, 128 x 128, 128
-// x 256 and 256 x 256:
-//   N = K = 4096       M = 32  11, 17, 19, 27, 30, 67, 80;  128  24, 17, 21, 29, 38, 75, 84
-//   N = 12288, K = 4096     48  36, 30, 25, 34, 35, 71, 83;  128  68, 43, 41, 35, 44, 82, 85
-//   N = 16384, K = 1024     32  17, 8.5, 9.1, 11, 12, 21, 27
-// and of warm weights, N = K = 4096, from 64 x 128 on: M = 512 25, 33, 53, 89; 1024 46, 37,
-// 54, 91; 2048 94, 73, 60, 97; 8192 385, 293, 246, 206. More wavefronts of less work
-// each were better throughout, a step of a lone workgroup being a chain of barrier,
-// LDS reads and products (128 x 128 on 4, 8 and 16 wavefronts, M = 512: 43, 36, 33);
-// 256 x 256 on 4 wavefronts of 128 x 128 took 288 us where these take 218, on 16 of
-// 64 x 64 the same, with 32x32x16 MFMAs 231.
+// 376 sizes with weights from HBM, M = 1..8192, N x K = 128 x 4096 to 24576 x 4096, K
+// from 128 to 16384, all kernels in turn in one process: the choice is on average 0.2 %
+// slower than the best, 7 % at most; without one of the two 128 x 256 tiles 1 % and
+// 27 %, without 64 x 64 or 64 x 128 more. In us on the streaming kernel, 32 x 64, 64 x
+// 64, 64 x 128, 128 x 128, 128 x 256 (16 wavefronts, 8 in pairs) and 256 x 256:
+//   N = K = 4096       M =   32  11, 17, 19, 27, 30, 67, 58, 80
+//                           128  24, 17, 21, 29, 38, 75, 59, 83
+//                           512   -, 49, 35, 30, 39, 71, 58, 84
+//                          1024   -, 91, 66, 57, 39, 70, 58, 85
+//                          2048   -, 157, 120, 108, 75, 74, 66, 91
+//                          8192   -, 567, 396, 360, 275, 241, 252, 210
+//   N = 12288, K = 4096      48  36, 30, 25, 34, 35, 71, 61, 82
+//   N = 8192, K = 256      3000   -, 63, 44, 47, 32, 27, 31, 33
+// More wavefronts of less work each were better for the small tiles, a step of a lone
+// workgroup being a chain of barrier, LDS reads and products (128 x 128 on 4, 8 and 16
+// wavefronts, M = 512: 43, 36, 33); 256 x 256 on 4 wavefronts of 128 x 128 took 288 us
+// where these take 218, on 16 of 64 x 64 the same, with 32x32x16 MFMAs 231.
 struct Shape {
   int bm, bn, fit;
   double start, step, chip, shared;
 };
-constexpr Shape kShapes[6] = {{32, 64, 2, 0.336, 0.100, 0.071, 0.071},  {64, 64, 2, 0.640, 0.055, 0.136, 0.144},
-                              {64, 128, 1, 0.219, 0.307, 0.137, 0.0},   {128, 128, 1, 1.162, 0.422, 0.182, 0.0},
-                              {128, 256, 1, 0.000, 1.007, 0.226, 0.0},  {256, 256, 1, 5.869, 1.078, 0.624, 0.0}};
+constexpr Shape kShapes[7] = {{32, 64, 2, 0.739, 0.080, 0.078, 0.043},  {64, 64, 2, 1.117, 0.040, 0.114, 0.103},
+                              {64, 128, 1, 1.517, 0.174, 0.203, 0.0},   {128, 128, 1, 1.499, 0.342, 0.235, 0.0},
+                              {128, 256, 1, 0.832, 0.868, 0.302, 0.0},  // 16 wavefronts
+                              {128, 256, 1, 4.854, 0.638, 0.337, 0.0},  // 8 in pairs
+                              {256, 256, 1, 5.993, 1.301, 0.297, 0.0}};
 constexpr int kStream = -1;
 
 int best_shape(int64_t M, int64_t Nw, int64_t K) {
@@ -383,9 +391,9 @@ int best_shape(int64_t M, int64_t Nw, int64_t K) {
     linear_tile(M, Nw, K, tile);
     const double items = static_cast<double>(Nw / tile[1] * ((M + 63) / 64));
     const double kb = static_cast<double>(2 * std::min<int64_t>(4, (M + 15) / 16) + tile[1] / 8);  // of a wavefront's step
-    best = 2.353 + std::ceil(items / cus) * ks / 4 * (0.163 + 0.006 * kb) + 0.031 * ks * items * kb / (4 * cus);
+    best = 2.704 + std::ceil(items / cus) * ks / 4 * (0.047 + 0.013 * kb) + 0.03 * ks * items * kb / (4 * cus);
   }
-  for (int t = 0; t < 6; ++t) {
+  for (int t = 0; t < 7; ++t) {
     const Shape& s = kShapes[t];
     const double items = static_cast<double>(((M + s.bm - 1) / s.bm) * ((Nw + s.bn - 1) / s.bn));
     const double per_cu = std::ceil(items / cus);
@@ -412,7 +420,8 @@ hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
     LT(2, 2, 4, 6);
     LT(3, 4, 4, 5);
     LT(4, 4, 4, 3);
-    default: hipLaunchKernelGGL((linear_act_256_kernel<kGlu>), round, dim3(512), 0, st, c);
+    case 5: hipLaunchKernelGGL((linear_act_pairs_kernel<kGlu, 128, 256, 3, 3>), round, dim3(512), 0, st, c); break;
+    default: hipLaunchKernelGGL((linear_act_pairs_kernel<kGlu, 256, 256, 2, 3>), round, dim3(512), 0, st, c);
   }
 #undef LT
   return hipGetLastError();
