@@ -476,8 +476,9 @@ int lacache_linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile)
  * int32); sequences may share pages. kv_heads divides heads; query head h reads
  * KV head h / (heads / kv_heads).
  * Limits (LACACHE_ERR_UNSUPPORTED otherwise): d 64 or 128; page 16, 32, 64, 128
- * or 256; heads <= 4096, S <= 4096, max_pages page <= 2^22, num_pages < 2^31, T
- * <= 2^24, nq <= 64. Sizes that are not positive (S, T: negative) and other
+ * or 256; heads <= 4096 (of the append: with 2 kv_heads), S <= 4096, max_pages
+ * page <= 2^22, num_pages < 2^31, T < 2^24, nq <= 64, S kv_heads ceil(nq heads /
+ * (16 kv_heads)) <= 2^23. Sizes that are not positive (S, T: negative) and other
  * cache types are LACACHE_ERR_INVALID_ARG.
  * Page numbers, positions and lengths are device data that the host cannot
  * check; what the kernels do with values out of range is said at each call, and

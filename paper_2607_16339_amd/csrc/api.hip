@@ -271,6 +271,12 @@ int ffn_core(hipStream_t st, const uint16_t* x, const uint16_t* y, const uint16_
 constexpr int64_t kPagedMaxSeqs = 4096;
 constexpr int64_t kPagedMaxTokens = int64_t(1) << 22;  // of a sequence
 constexpr int64_t kPagedMaxNq = 64;
+// (the threads of a launch are counted in 32 bits: 256 for a token, or for a sequence, KV head and row tile)
+constexpr int64_t kPagedMaxAppend = (int64_t(1) << 24) - 1;
+constexpr int64_t kPagedMaxGroups = int64_t(1) << 23;
+bool paged_groups_ok(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads) {
+  return S * kv_heads * ((nq * (heads / kv_heads) + 15) / 16) <= kPagedMaxGroups;
+}
 int check_heads(int64_t heads, int64_t kv_heads, int64_t d) {
   if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0 || d <= 0) return LACACHE_ERR_INVALID_ARG;
   return heads > kAttnMaxHeads || (d != 64 && d != 128) ? LACACHE_ERR_UNSUPPORTED : LACACHE_OK;
@@ -298,7 +304,7 @@ int check_attention(const uint16_t* q, const void* k_cache, const void* v_cache,
                     int64_t max_pages, float scale, int causal, int cache_type, PagedAttn* a) {
   RETURN_IF(check_paged(S, max_pages, num_pages, page, heads, kv_heads, d, cache_type));
   if (nq <= 0 || causal < 0 || causal > 1 || !(scale >= 0.0f) || scale > 3.0e38f) return LACACHE_ERR_INVALID_ARG;
-  if (nq > kPagedMaxNq) return LACACHE_ERR_UNSUPPORTED;
+  if (nq > kPagedMaxNq || !paged_groups_ok(S, nq, heads, kv_heads)) return LACACHE_ERR_UNSUPPORTED;
   if (S == 0) return LACACHE_OK;
   const bool fp8 = cache_type == LACACHE_KV_E4M3;
   if (!ptrs_ok({q, k_cache, v_cache, page_table, seq_lens, o}) || !opt_ptr_ok(lse)) return LACACHE_ERR_INVALID_ARG;
@@ -799,7 +805,7 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
   RETURN_IF(check_paged(S, max_pages, num_pages, page, heads, kv_heads, d, cache_type));
   if (T < 0 || rope_dim < 0 || rope_dim % 16 != 0 || rope_dim > d || (rope_dim > 0 && rope_len <= 0))
     return LACACHE_ERR_INVALID_ARG;
-  if (T > kMaxM || heads + 2 * kv_heads > kAttnMaxHeads) return LACACHE_ERR_UNSUPPORTED;
+  if (T > kPagedMaxAppend || heads + 2 * kv_heads > kAttnMaxHeads) return LACACHE_ERR_UNSUPPORTED;
   if (T == 0 || S == 0) return LACACHE_OK;
   const bool fp8 = cache_type == LACACHE_KV_E4M3, rot = rope_dim > 0;
   if (!ptrs_ok({qkv, seq_ids, positions, page_table, q, k_cache, v_cache})) return LACACHE_ERR_INVALID_ARG;
@@ -829,7 +835,8 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
 }
 
 size_t lacache_paged_attention_workspace_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
-  if (S < 0 || S > kPagedMaxSeqs || nq <= 0 || nq > kPagedMaxNq || check_heads(heads, kv_heads, d) != LACACHE_OK)
+  if (S < 0 || S > kPagedMaxSeqs || nq <= 0 || nq > kPagedMaxNq || check_heads(heads, kv_heads, d) != LACACHE_OK ||
+      !paged_groups_ok(S, nq, heads, kv_heads))
     return 0;
   return paged_attention_ws_bytes(S, nq, heads, kv_heads, d);
 }

@@ -120,6 +120,22 @@ def test_skipped_tokens_leave_everything_as_it_was(fp8):
     c.check("skipped")
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("heads,kv,d", [(32, 8, 128), (16, 8, 64), (1, 1, 64), (9, 3, 128)])
+def test_skipped_tokens_among_others(heads, kv, d, fp8):
+    # whole workgroups of a token, and workgroups of several tokens
+    toks = [(-1 if i % 3 == 1 else i % 2, -1 if i % 7 == 2 else i // 2) for i in range(101)]
+    c = Call(2, toks, heads, kv, d, 16, fp8, d, seed=heads, rope_len=45)
+    c.table[1, 1] = -1
+    c.check("skipped among others")
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,heads,kv,d", [(1501, 1, 1, 64), (701, 4, 1, 64), (777, 5, 5, 128), (1100, 14, 2, 64), (600, 24, 12, 128)])
+def test_many_tokens_of_few_heads(T, heads, kv, d, fp8):
+    Call(3, [(i % 3, i // 3) for i in range(T)], heads, kv, d, 128, fp8, 32, max_pages=4, seed=T).check("T %d heads %d" % (T, heads))
+
+
 def test_zeros_and_values_that_are_no_numbers():
     c = Call(1, [(0, i) for i in range(6)], 2, 1, 64, 16, True, 0, seed=4)
     x = c.qkv.view(6, 4, 64)

@@ -54,7 +54,7 @@ def test_append_refusals(L):
         assert _append(L, **bad) == INVALID, bad
     for bad in (dict(d=96), dict(d=256, rope_dim=128), dict(page=8), dict(page=48), dict(page=512), dict(S=4097),
                 dict(max_pages=(1 << 18) + 1), dict(num_pages=1 << 31), dict(T=(1 << 24) + 1),
-                dict(heads=4096, kv=8)):
+                dict(T=1 << 24), dict(heads=4096, kv=8)):
         assert _append(L, **bad) == UNSUP, bad
     assert _append(L, T=0, rope_dim=0, cos=None, sin=None, rope_len=0) == OK
 
@@ -76,7 +76,8 @@ ATTN_INVALID = (dict(S=-1), dict(nq=0), dict(nq=-1), dict(heads=0), dict(kv=0), 
                 dict(lse=_addr(1)), dict(lse=_addr(5)), dict(ks=_addr(9)), dict(kind=1), dict(kind=1, vs=_addr(9)),
                 dict(kind=1, ks=_addr(9), vs=_addr(10) + 8), dict(kind=1, ks=_addr(9), vs=_addr(10), o=_addr(10)))
 ATTN_UNSUP = (dict(nq=65), dict(d=96), dict(d=256), dict(page=1), dict(page=24), dict(page=512), dict(S=4097),
-              dict(heads=8192), dict(max_pages=(1 << 18) + 1), dict(num_pages=1 << 31))
+              dict(heads=8192), dict(max_pages=(1 << 18) + 1), dict(num_pages=1 << 31),
+              dict(S=4096, heads=4096, kv=4096), dict(S=4096, heads=2056, kv=2056), dict(S=4096, nq=64, heads=1032, kv=8))
 
 
 def test_attention_refusals(L):
@@ -98,7 +99,8 @@ def test_attention_workspace_refusals(L):
     for bad in ATTN_INVALID:
         assert _attn(L, **ws(_addr(9) + (1 << 35), 1 << 34), **bad) == INVALID, bad
     for bad in ((-1, 1, 32, 8, 128), (2, 0, 32, 8, 128), (2, 65, 32, 8, 128), (2, 1, 30, 8, 128), (2, 1, 32, 8, 96),
-                (4097, 1, 32, 8, 128), (2, 1, 0, 0, 128)):
+                (4097, 1, 32, 8, 128), (2, 1, 0, 0, 128),
+                (4096, 1, 4096, 4096, 64)):
         assert L.lacache_paged_attention_workspace_bytes(*bad) == 0, bad
 
 
