@@ -184,11 +184,14 @@ __device__ __forceinline__ int total_tiles(const PagedAttn& a, int lane, int fir
 // twice Wq of them, for balance. Shorter ones: the least length, from kLeast, at
 // which all pieces run at once, if one below kLong does that. A sequence of at most
 // kWhole tiles stays whole: a second kernel costs more than its few steps.
-// kWays: wavefronts that split a piece's keys; 1: they split its rows, and a piece's
-// state is 128 rows, eight tiles' worth of bytes.
+// kWays: wavefronts that split a piece's keys. 1: they split its rows, every tile is a
+// step of 2 us for each, and shorter pieces pay although a piece's state is 128 rows:
+// with the least 8 and whole up to 12 tiles, against 2 and 4, 72 rows over 8 sequences of
+// 1..899 keys (D = 64) take 39 us against 18.6, 224 rows of 300 keys 18.0 / 13.7, over 8
+// sequences of 200..1024 27 / 24 (128 rows over 2 of 4096 24.5 / 26.5).
 template <int kWays>
 struct PieceRule {
-  static constexpr int kLeast = 8, kWhole = kWays > 1 ? 32 : 12, kLong = 64;
+  static constexpr int kLeast = kWays > 1 ? 8 : 2, kWhole = kWays > 1 ? 32 : 4, kLong = 64;
 };
 template <int kKeys, int kWays>
 __device__ __forceinline__ int piece_tiles(const PagedAttn& a, int lane, int first) {
@@ -751,13 +754,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 // More than 64 rows: four wavefronts of 32 rows each share every tile of keys, which
 // comes in stages of kTiles tiles (16 KB of keys, 16 of values) through two LDS
 // buffers, each wavefront copying its share; one barrier per stage. The products and
-// the softmax bound these calls, not the stream (208 rows: 215 TFLOP/s). Against row
-// tiles of 32 whose wavefronts split the keys (8 sequences of 1000..4096 keys, 8 KV
-// heads, D = 128): 72 rows 38.2 us against 43.9, 96 39.4 / 44.3, 128 42.5 / 43.6,
-// 256 78.4 / 87.4; 64 sequences of 128 rows and 500..1024 keys 71.6 / 89.6. For up
-// to 64 rows two row tiles of 32 are the better choice: 19.1 us against 21.9 for 8
-// sequences of 1000 keys, 67 / 86 for one of 65536, 96 / 111 for 32 of 1000..4096
-// (two wavefronts of 32 rows instead of four: 22.2, 92 and 86).
+// the softmax bound these calls, not the stream: the matrix cores are busy 30 % of the
+// time (P's second term counted), the vector units 50 % (224 rows over 8 sequences of
+// 4000 keys, 360 TFLOP/s), and two wavefronts per SIMD overlap little more than that.
+// Against row tiles of 32 whose wavefronts split the keys (8 sequences of 1000..4096
+// keys, 8 KV heads, D = 128): 72 rows 35.7 us against 42.9, 96 37.8 / 43.7, 128 41.1 /
+// 46.1, 256 76 / 86; one sequence of 65536 and 96 rows 90 / 118; 64 sequences of 128
+// rows and 500..1024 keys 70 / 88. For up to 64 rows two row tiles of 32 are the better
+// choice: 16.0 us against 21.7 for 8 sequences of 1000 keys, 67.9 / 70.7 for one of
+// 65536, 96 / 104 for 32 of 1000..4096; two wavefronts of 32 rows were no better
+// (22.2, 92 and 86).
 template <int D, bool kFp8>
 __global__ __launch_bounds__(256, 2) void paged_attention_rows_kernel(PagedAttn a) {
   constexpr int RG = 4;
@@ -1007,8 +1013,7 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     using Rows = PieceRule<1>;
     const int64_t nt = (a.max_len + keys - 1) / keys;
     const int64_t whole = p.wq <= a.S ? Keys::kLong : (p.ways > 1 ? Keys::kWhole : Rows::kWhole);
-    const int64_t least = Keys::kLeast;
-    static_assert(Keys::kLeast == Rows::kLeast, "one bound for both");
+    const int64_t least = p.ways > 1 ? Keys::kLeast : Rows::kLeast;
     if (p.wq == 1 || nt <= whole) return static_cast<int64_t>(a.S);
     return std::min(2 * p.wq + a.S, a.S * ((nt + least - 1) / least));
   };
