@@ -755,8 +755,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 // comes in stages of kTiles tiles (16 KB of keys, 16 of values) through two LDS
 // buffers, each wavefront copying its share; one barrier per stage. The products and
 // the softmax bound these calls, not the stream: the matrix cores are busy 30 % of the
-// time (P's second term counted), the vector units 50 % (224 rows over 8 sequences of
-// 4000 keys, 360 TFLOP/s), and two wavefronts per SIMD overlap little more than that.
+// time (P's second term counted), the vector units 50 % (256 rows over 8 sequences of
+// 4000 keys, 350 TFLOP/s), and two wavefronts per SIMD overlap little more than that.
 // Against row tiles of 32 whose wavefronts split the keys (8 sequences of 1000..4096
 // keys, 8 KV heads, D = 128): 72 rows 35.7 us against 42.9, 96 37.8 / 43.7, 128 41.1 /
 // 46.1, 256 76 / 86; one sequence of 65536 and 96 rows 90 / 118; 64 sequences of 128
