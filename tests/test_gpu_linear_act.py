@@ -151,6 +151,19 @@ def test_rows_do_not_depend_on_the_call(act):
     assert len(seen) >= 4
 
 
+@pytest.mark.parametrize("act", [NONE, SWIGLU])
+def test_rows_do_not_depend_on_the_call_at_a_longer_k(act):
+    a, w, b, r = _case(8192, 1024, 4096, act, True, True, seed=5)
+    seen, first = set(), None
+    for M in (129, 700, 1500, 3000, 4096, 8192):
+        out = torch.empty((M, 1024), dtype=torch.bfloat16, device=DEV)
+        lc.lacache_linear_act_bf16(a[:M], w, out, bias=b, residual=r[:M], act=act)
+        seen.add(lc.lacache_linear_act_tile(M, 1024, 4096, act))
+        first = out[:129].clone() if first is None else first
+        assert torch.equal(out[:129].view(torch.int16), first.view(torch.int16)), M
+    assert (128, 256) in seen and len(seen) >= 3
+
+
 @pytest.mark.parametrize("M", [1, 16, 33, 64, 100, 128])
 def test_streamed_product_is_the_plain_one_bit_for_bit(M):
     assert lc.lacache_linear_act_tile(M, 1024, 4096)[1] in (16, 48)
