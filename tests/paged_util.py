@@ -7,7 +7,9 @@ factors (3 u |s|); with the exponential's argument in fp32 and the hardware
 exp2 (2 u relative) a p is off by e_p = (d + 4) u scale sum|q k| + 4 u |s - m| + 4 u,
 relatively. P enters the value product as two bf16 terms (2^-16 relative) and
 the n products are summed in fp32 (n u of sum p |v|), as is l. Splitting the
-keys multiplies a part by another exponential (4 u + 2 u |s - m|). So
+keys multiplies a part by another exponential (4 u + 2 u |s - m|). The base may lie
+up to 8 (in powers of 2) below m: an argument's rounding then grows by 8 u, a p by
+8 u ln 2, the quotient of two sums by less than 2^-20, the last term. So
   |o - ref| <= 2^-8 |ref| + (2 max e_p + 2^-16 + 2 n u + 2^-20) sum p |v| / l,
 the first term the one rounding to bf16, and
   |lse - ref| <= max e_p + n u + 2^-20 + 2^-22 |ref|.

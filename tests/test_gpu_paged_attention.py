@@ -260,6 +260,44 @@ def test_captured_and_replayed_with_growing_lengths():
         assert torch.equal(_bits(got), _bits(want)), sub
 
 
+@pytest.mark.parametrize("nq", [1, 12, 20])  # 4, 48 and 80 rows per KV head
+def test_captured_and_replayed_with_cuts_that_move(nq):
+    """Two graphs on one workspace; their sequences go from many pieces to one and back."""
+    c = Cache([9000, 2500, 64], 8, 2, 128, 16, False, seed=23)
+    q, full = _q(c, nq), c.lens.clone()
+    ws = torch.empty(lc.lacache_paged_attention_workspace_bytes(3, nq, 8, 2, 128), dtype=torch.uint8, device=DEV)
+    attend(c, q, True, workspace=ws)
+    torch.cuda.synchronize()
+    outs, graphs = [torch.empty_like(q) for _ in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for o, graph, causal in zip(outs, graphs, (True, False)):
+        with torch.cuda.graph(graph):
+            lc.lacache_paged_attention(q, c.k, c.v, c.table, c.lens, o, causal=causal, workspace=ws)
+    for lens in (full.tolist(), [100, 2500, 0], [9000, 0, 64], [1, 1, 1], [4000, 2000, 33], full.tolist()):
+        c.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for o, causal in zip(outs, (True, False)):
+            got = o.clone()
+            want, _ = attend(c, q, causal)
+            torch.cuda.synchronize()
+            assert torch.equal(_bits(got), _bits(want)), (lens, causal)
+
+
+@pytest.mark.parametrize("nq,heads,kv", [(1, 8, 2), (20, 8, 2), (40, 2, 2), (20, 32, 8)])
+@pytest.mark.parametrize("S,longest", [(1, 20000), (3, 1100), (20, 1100), (50, 140), (120, 140), (127, 2100)])
+def test_workspace_is_as_large_as_it_is_said_to_be(S, longest, nq, heads, kv):
+    """What lies behind the workspace stays; lengths just above those that are not cut."""
+    c = Cache([longest - (i % 5) * (longest // 50) for i in range(S)], heads, kv, 64, 16, True, seed=S)
+    q = _q(c, nq)
+    n = lc.lacache_paged_attention_workspace_bytes(S, nq, heads, kv, 64)
+    buf = torch.full((n + (1 << 20),), 0xAB, dtype=torch.uint8, device=DEV)
+    o, _ = attend(c, q, False, workspace=buf[:n])
+    want, _ = attend(c, q, False)
+    torch.cuda.synchronize()
+    assert bool((buf[n:] == 0xAB).all()) and torch.equal(_bits(o), _bits(want))
+
+
 def test_two_streams_with_their_own_workspaces():
     cs = [Cache([3000, 100 + i], 8, 2, 128, 16, False, seed=20 + i) for i in range(2)]
     qs = [_q(c, 1, seed=i) for i, c in enumerate(cs)]
