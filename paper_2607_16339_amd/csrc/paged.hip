@@ -519,9 +519,7 @@ struct PagedRows {
         m[x] = mn;
         l[x] *= alpha;
 #pragma unroll
-        for (int d = 0; d < kDims; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) ot[x][d][e] *= alpha;
+        for (int d = 0; d < kDims; ++d) ot[x][d] *= alpha;
       }
     }
 #pragma unroll
@@ -550,11 +548,17 @@ struct PagedRows {
 #pragma unroll
         for (int x = 0; x < RT; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = sc[x][tt][e] * vs[e];
-            // (a hidden key's scale may be no number)
-            sc[x][tt][e] = (!whole || differ) && hidden(cnt, key0, x, tt, e) ? 0.0f : p;
-          }
+          for (int e = 0; e < 4; ++e) sc[x][tt][e] *= vs[e];
+      }
+      if (!whole || differ) {
+        asm volatile("" ::: "memory");  // (one branch around all of it)
+        // a hidden key's scale may be no number
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+          for (int tt = 0; tt < kSub; ++tt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[x][tt][e] = hidden(cnt, key0, x, tt, e) ? 0.0f : sc[x][tt][e];
       }
     }
     bf8 ph[RT][kKeys / 32], pl[RT][kKeys / 32];
@@ -628,8 +632,7 @@ struct PagedRows {
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
               const v4f sum = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
-#pragma unroll
-              for (int e = 0; e < 4; ++e) ot[x][d][e] = key < limit[x] ? sum[e] : ot[x][d][e];
+              ot[x][d] = key < limit[x] ? sum : ot[x][d];
             }
           }
         }
