@@ -140,8 +140,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int64_
 // one product per key, whose result the hiding rows do not take.
 //
 // Measured (32 heads over 8 KV heads, D = 128; a large copy moves 5.05 TB/s): 48
-// sequences of 1..8191 keys, bf16, 157 us = 5.3 TB/s; 64 of 12000..16384, e4m3, 64
-// heads, 368 us = 5.2 TB/s; one of 131072, e4m3, 59 us = 4.7 TB/s; one of 500, 9.4 us
+// sequences of 1..8191 keys, bf16, 155 us = 5.4 TB/s; 64 of 12000..16384, e4m3, 64
+// heads, 364 us = 5.3 TB/s; one of 131072, e4m3, 58 us = 4.8 TB/s; one of 500, 8.6 us
 // with the call's way through the host, the chain of loads length - page - keys -
 // values being what its kernel waits for.
 // ---------------------------------------------------------------------------
