@@ -319,8 +319,10 @@ __device__ __forceinline__ int64_t out_row(const PagedAttn& a, int s, int h, int
   return (static_cast<int64_t>(s) * a.nq + t) * a.heads + h * G + (rr - t * G);
 }
 
+// (a row without any weight is 0 also where its O is no number: 0 times an infinite value)
 __device__ __forceinline__ void store_out(const PagedAttn& a, int64_t row, int D, int c4, v4f o, float m, float l) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (l == 0.0f) o = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   *reinterpret_cast<uint2*>(a.o + row * D + 4 * c4) =
       make_uint2(cvt_pk_bf16(o[0] * inv, o[1] * inv), cvt_pk_bf16(o[2] * inv, o[3] * inv));
   if (a.lse != nullptr && c4 == 0) a.lse[row] = (m + __log2f(l)) * 0.69314718055994531f;

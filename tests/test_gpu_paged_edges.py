@@ -1,0 +1,62 @@
+"""Attention over the paged cache at the places where a key can be lost or a
+value leak: rows that every score hides, values that are no numbers in causal
+tiles. Each form of the kernel is reached by its number of rows per KV head and
+by its number of sequences (FORMS)."""
+
+import math
+
+import pytest
+import torch
+
+from paged_util import DEV, Cache, attend, normal
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+# (nq, heads, kv): 8, 16 rows per KV head (one row tile), 40 (two), 80 and 208 (wavefronts that split the rows)
+FORMS = [(8, 1, 1), (8, 4, 2), (20, 2, 1), (40, 2, 1), (26, 16, 2)]
+
+
+def _q(c, nq, seed=1, std=1.5):
+    return normal(torch.Generator().manual_seed(seed), (c.S, nq, c.heads, c.d), std).to(DEV)
+
+
+def _bits(t):
+    return t.view(torch.int16) if t.dtype == torch.bfloat16 else t.view(torch.int32)
+
+
+def _place(c, s, key):
+    return int(c.table[s, key // c.page]), key % c.page
+
+
+def _put_value(c, s, key, head, dim, x):
+    """Value `key` of sequence s in dimension `dim` becomes x (of an e4m3 cache: NaN)."""
+    page, slot = _place(c, s, key)
+    if c.fp8:
+        c.v.view(torch.uint8)[page, head, slot, dim] = 0x7F
+    else:
+        c.v[page, head, slot, dim] = x
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,heads,kv", FORMS)
+def test_rows_whose_scores_are_all_minus_infinity_take_no_value(nq, heads, kv, d, fp8):
+    """o = 0 and lse = -inf whatever the values hold, of whole sequences and of cut ones."""
+    lens = [60, 4500, 333]
+    c = Cache(lens, heads, kv, d, 16, fp8, seed=nq + d)
+    q = _q(c, nq).abs().clamp_min(0.125)  # (-inf times 0 would be none)
+    for s in (0, 1):
+        pages = c.table[s, : -(-lens[s] // 16)].long()
+        if fp8:
+            c.k.view(torch.uint8)[pages] = 0x38  # 1.0
+            c.k_scale[pages] = -INF
+        else:
+            c.k[pages] = -INF
+        for key, x in ((3, INF), (lens[s] // 2, NAN), (lens[s] - 1, -INF)):
+            for h in range(kv):
+                _put_value(c, s, key, h, 7, x)
+    o, lse = attend(c, q, False)
+    torch.cuda.synchronize()
+    assert bool((o[:2] == 0).all()) and bool((lse[:2] == -math.inf).all())
+    assert bool(torch.isfinite(o[2].float()).all()) and bool(torch.isfinite(lse[2]).all())
