@@ -136,8 +136,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppend a, int64_
 //
 // Places that no row may see: keys behind the end or on no page get scores of
 // -inf and value rows of zeros in LDS (0 times a NaN would be one); in the tiles
-// where causal rows differ, values that are not finite send the tile through
-// one product per key, whose result the hiding rows do not take.
+// where causal rows differ, values that are not finite send the tile through one
+// product per number of keys that a row sees, with zeros for the values behind.
 //
 // Measured (32 heads over 8 KV heads, D = 128; a large copy moves 5.05 TB/s): 48
 // sequences of 1..8191 keys, bf16, 155 us = 5.4 TB/s; 64 of 12000..16384, e4m3, 64
@@ -617,28 +617,35 @@ struct PagedRows {
           for (int x = 0; x < RT; ++x) ot[x][d] = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
         }
     } else {
-#pragma unroll
-      for (int st = 0; st < kKeys / 32; ++st)
+      // For each number n of the tile's keys that a row may see: the products above with zeros
+      // for the values behind, which only the rows that see n take. In those rows P is zero
+      // there, so every bit is as with values that are finite.
 #pragma unroll 1
-        for (int kk = 0; kk < 32; ++kk) {
-          // key kk of the step: element 4 (kk / 16) + kk % 4 of the lanes of group (kk / 4) % 4
-          const int el = 4 * (kk >> 4) + (kk & 3), key = key0 + 32 * st + kk;
-          const bool mine = g == ((kk >> 2) & 3);
+      for (int n = 1; n <= kKeys; ++n) {
 #pragma unroll
-          for (int d = 0; d < kDims; ++d) {
+        for (int d = 0; d < kDims; ++d) {
+          __builtin_amdgcn_sched_barrier(0);  // (one at a time: few registers are left)
+          v4f sum[RT];
+#pragma unroll
+          for (int x = 0; x < RT; ++x) sum[x] = ot[x][d];
+#pragma unroll
+          for (int st = 0; st < kKeys / 32; ++st) {
             const uint4 w = __builtin_bit_cast(uint4, value_operand(Vt, vb, st, d));
             uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            const int left = fresh(n - 4 * g) - 32 * st;  // (words e / 2: keys 16 (e / 2) + 2 (e % 2) and the next)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              ww[e] = mine && (el >> 1) == e ? (el & 1 ? ww[e] & 0xFFFF0000u : ww[e] & 0xFFFFu) : 0u;
+            for (int e = 0; e < 4; ++e) {
+              const int k = 16 * (e >> 1) + 2 * (e & 1);
+              ww[e] = k + 1 < left ? ww[e] : (k < left ? ww[e] & 0xFFFFu : 0u);
+            }
             const bf8 vf = __builtin_bit_cast(bf8, make_uint4(ww[0], ww[1], ww[2], ww[3]));
 #pragma unroll
-            for (int x = 0; x < RT; ++x) {
-              const v4f sum = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], ot[x][d]));
-              ot[x][d] = key < limit[x] ? sum : ot[x][d];
-            }
+            for (int x = 0; x < RT; ++x) sum[x] = mfma16(vf, pl[x][st], mfma16(vf, ph[x][st], sum[x]));
           }
+#pragma unroll
+          for (int x = 0; x < RT; ++x) ot[x][d] = fresh(min(limit[x] - key0, kKeys)) == n ? sum[x] : ot[x][d];
         }
+      }
     }
   }
 

@@ -60,3 +60,28 @@ def test_rows_whose_scores_are_all_minus_infinity_take_no_value(nq, heads, kv, d
     torch.cuda.synchronize()
     assert bool((o[:2] == 0).all()) and bool((lse[:2] == -math.inf).all())
     assert bool(torch.isfinite(o[2].float()).all()) and bool(torch.isfinite(lse[2]).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,heads,kv", FORMS)
+@pytest.mark.parametrize("length,key", [(128, 125), (128, 67), (4992, 4989)])
+def test_values_of_hidden_keys_move_no_bit(length, key, nq, heads, kv, d, fp8):
+    """A value that is no number late in a tile: causal rows before it keep every bit, although
+    they see other keys of its tile; rows that see it keep every other dimension's."""
+    c = Cache([length, 70], heads, kv, d, 16, fp8, seed=length + d)
+    q = _q(c, nq)
+    want, wl = attend(c, q, True)
+    for dim, x in ((5, NAN), (d - 2, INF), (5, -INF)):
+        old = c.v.view(torch.uint8).clone()
+        for h in range(kv):
+            _put_value(c, 0, key, h, dim, x)
+        o, lse = attend(c, q, True)
+        torch.cuda.synchronize()
+        c.v.view(torch.uint8).copy_(old)
+        sees = [t for t in range(nq) if key <= length - nq + t]
+        assert torch.equal(_bits(lse), _bits(wl)), (dim, x)
+        keep = torch.ones(o.shape, dtype=torch.bool, device=DEV)
+        keep[0, sees, :, dim] = False
+        assert torch.equal(_bits(o)[keep], _bits(want)[keep]), (dim, x)
+        assert not bool(torch.isfinite(o.float())[~keep].any()), (dim, x)
