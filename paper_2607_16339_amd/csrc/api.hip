@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
@@ -303,7 +304,8 @@ int check_attention(const uint16_t* q, const void* k_cache, const void* v_cache,
                     int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d, int64_t num_pages, int64_t page,
                     int64_t max_pages, float scale, int causal, int cache_type, PagedAttn* a) {
   RETURN_IF(check_paged(S, max_pages, num_pages, page, heads, kv_heads, d, cache_type));
-  if (nq <= 0 || causal < 0 || causal > 1 || !(scale >= 0.0f) || scale > 3.0e38f) return LACACHE_ERR_INVALID_ARG;
+  const float scale_log2 = scale * 1.4426950408889634f;  // the kernels' factor (base 2)
+  if (nq <= 0 || causal < 0 || causal > 1 || !(scale >= 0.0f) || std::isinf(scale_log2)) return LACACHE_ERR_INVALID_ARG;
   if (nq > kPagedMaxNq || !paged_groups_ok(S, nq, heads, kv_heads)) return LACACHE_ERR_UNSUPPORTED;
   if (S == 0) return LACACHE_OK;
   const bool fp8 = cache_type == LACACHE_KV_E4M3;
@@ -323,7 +325,7 @@ int check_attention(const uint16_t* q, const void* k_cache, const void* v_cache,
   a->S = static_cast<int>(S), a->nq = static_cast<int>(nq), a->heads = static_cast<int>(heads);
   a->kv_heads = static_cast<int>(kv_heads), a->page_log2 = log2_of(page);
   a->max_len = static_cast<int>(max_pages * page), a->causal = causal;
-  a->scale_log2 = scale * 1.4426950408889634f;
+  a->scale_log2 = scale_log2;
   return LACACHE_OK;
 }
 
