@@ -537,7 +537,8 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
  * cut into pieces whose sums are joined; where the cuts lie depends on the lengths of
  * the call, so a row's last bits may differ between batches (the same inputs
  * give the same bytes). S == 0 launches nothing. Uses the library workspace
- * like lacache_ffn_fp8 (the same rules of order and capture).
+ * like lacache_ffn_fp8 (the same rules of order and capture): as much of it as
+ * sequences that fill the table would need, and none where such are not cut.
  */
 int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,
                             const float* k_scale, const float* v_scale, const int32_t* page_table,
@@ -546,7 +547,7 @@ int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache
                             float scale, int causal, int cache_type);
 
 /* Bytes of workspace that lacache_paged_attention_ws needs on the current
- * device (0 on bad arguments). */
+ * device, whatever the table's length (0 on bad arguments). */
 size_t lacache_paged_attention_workspace_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
 
 /* lacache_paged_attention with a caller-owned workspace of at least that size

@@ -853,9 +853,11 @@ int lacache_paged_attention(void* stream, const uint16_t* q, const void* k_cache
                             d, num_pages, page, max_pages, scale, causal, cache_type, &a));
   if (S == 0) return LACACHE_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool fp8 = cache_type == LACACHE_KV_E4M3;
+  const size_t need = paged_attention_need_bytes(a, d, fp8);
   void* ws = nullptr;
-  RETURN_IF(get_workspace(st, paged_attention_ws_bytes(S, nq, heads, kv_heads, d), &ws));
-  return hip_status(launch_paged_attention(st, a, d, cache_type == LACACHE_KV_E4M3, ws));
+  if (need > 0) RETURN_IF(get_workspace(st, need, &ws));
+  return hip_status(launch_paged_attention(st, a, d, fp8, ws));
 }
 
 int lacache_paged_attention_ws(void* stream, const uint16_t* q, const void* k_cache, const void* v_cache,

@@ -182,7 +182,10 @@ struct PagedAttn {
   int join_rows;  // of a workgroup of the join
   int whole;      // no sequence can have several pieces (the table is too short, or the heads are enough)
 };
+// The workspace of any such call, whatever its table, and of call a: less, and 0 (ws may
+// be null) where its table is so short that no sequence is cut.
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d);
+size_t paged_attention_need_bytes(const PagedAttn& a, int64_t d, bool fp8);
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws);
 
 }  // namespace lacache

@@ -269,11 +269,14 @@ __device__ __forceinline__ bool find_piece(const PagedAttn& a, int lane, Piece& 
   return false;  // (fewer pieces than the grid has room for)
 }
 
+// Keys of a tile, of rt tiles of 16 rows: 64, or 32 where 64 would not fit the LDS or the registers.
+constexpr int tile_keys(int d, bool fp8, int rt) {
+  return d * (fp8 ? 1 : 2) == 256 || (d == 128 && rt == 2) ? 32 : 64;
+}
 template <int D, bool kFp8, int RT>
 struct PagedTile {
   static constexpr int RB = D * (kFp8 ? 1 : 2);       // bytes of a key
-  // keys of a tile (32 also where 64 would not fit the registers)
-  static constexpr int kKeys = RB == 256 || (D == 128 && RT == 2) ? 32 : 64;
+  static constexpr int kKeys = tile_keys(D, kFp8, RT);
   static constexpr int kBytes = kKeys * RB;           // of an LDS slot
   static constexpr int CPR = RB / 16;                 // 16-byte chunks of a key
   static constexpr int KPI = 1024 / RB;               // keys of a copy instruction
@@ -1007,35 +1010,54 @@ hipError_t launch_paged_append(hipStream_t st, PagedAppend a, int64_t T, int64_t
 }
 
 // The workspace: [S] (pieces, first kept piece), then the kept pieces' states.
-static size_t cuts_bytes(int64_t S) { return (static_cast<size_t>(S) * 8 + 255) / 256 * 256; }
+static size_t ws_bytes(int64_t S, int64_t parts, int64_t rows, int64_t d) {
+  const size_t cuts = (static_cast<size_t>(S) * 8 + 255) / 256 * 256;
+  return (cuts + static_cast<size_t>(parts) * rows * (d + 2) * 4 + 255) / 256 * 256;
+}
 size_t paged_attention_ws_bytes(int64_t S, int64_t nq, int64_t heads, int64_t kv_heads, int64_t d) {
   const PagedPlan p = paged_plan(S, nq, heads, kv_heads);
-  const size_t bytes = cuts_bytes(S) + static_cast<size_t>(p.parts) * p.rows * (d + 2) * 4;
-  return (bytes + 255) / 256 * 256;
+  return ws_bytes(S, p.parts, p.rows, d);
+}
+
+namespace {
+// What the capacity of the table's pages leaves of a plan.
+struct PagedRoom {
+  int64_t pieces;  // of all sequences, at most; S: none can be cut
+  int64_t kept;    // piece states, at most
+};
+PagedRoom paged_room(const PagedPlan& p, const PagedAttn& a, int64_t d, bool fp8) {
+  using Keys = PieceRule<8>;
+  using Rows = PieceRule<1>;
+  const int keys = tile_keys(static_cast<int>(d), fp8, p.rows == 16 ? 1 : 2);
+  const int64_t nt = (a.max_len + keys - 1) / keys;
+  const int64_t whole = p.wq <= a.S ? Keys::kLong : (p.ways > 1 ? Keys::kWhole : Rows::kWhole);
+  const int64_t least = p.ways > 1 ? Keys::kLeast : Rows::kLeast;
+  if (p.wq == 1 || nt <= whole) return {a.S, 0};
+  const int64_t by_table = a.S * ((nt + least - 1) / least);  // (piece_tiles is never below kLeast)
+  return {std::min(2 * p.wq + a.S, by_table), std::min(p.parts, by_table * a.kv_heads * p.row_tiles)};
+}
+}  // namespace
+
+size_t paged_attention_need_bytes(const PagedAttn& a, int64_t d, bool fp8) {
+  const PagedPlan p = paged_plan(a.S, a.nq, a.heads, a.kv_heads);
+  const PagedRoom r = paged_room(p, a, d, fp8);
+  return r.pieces == a.S ? 0 : ws_bytes(a.S, r.kept, p.rows, d);
 }
 
 hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool fp8, void* ws) {
   const PagedPlan p = paged_plan(a.S, a.nq, a.heads, a.kv_heads);
-  a.cuts = static_cast<int2*>(ws);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cuts_bytes(a.S));
+  const int64_t n = paged_room(p, a, d, fp8).pieces;
+  a.whole = n == a.S;
+  if (!a.whole) {
+    a.cuts = static_cast<int2*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + ws_bytes(a.S, 0, 0, 0));
+  }
   a.row_tiles = static_cast<int>(p.row_tiles);
   a.wq = static_cast<int>(p.wq);
-  // pieces: as many as the lengths may ask for, and as the table's pages can hold
-  auto most_pieces = [&](int keys) {
-    using Keys = PieceRule<8>;
-    using Rows = PieceRule<1>;
-    const int64_t nt = (a.max_len + keys - 1) / keys;
-    const int64_t whole = p.wq <= a.S ? Keys::kLong : (p.ways > 1 ? Keys::kWhole : Rows::kWhole);
-    const int64_t least = p.ways > 1 ? Keys::kLeast : Rows::kLeast;
-    if (p.wq == 1 || nt <= whole) return static_cast<int64_t>(a.S);
-    return std::min(2 * p.wq + a.S, a.S * ((nt + least - 1) / least));
-  };
-  auto launch = [&](auto kernel, auto join, int keys) {
-    const int64_t n = most_pieces(keys);
-    a.whole = n == a.S;
+  auto launch = [&](auto kernel, auto join) {
     const dim3 grid(static_cast<unsigned>((n * a.kv_heads + 7) / 8 * 8 * p.row_tiles));
     hipLaunchKernelGGL(kernel, grid, dim3(p.ways == 8 ? 512 : 256), 0, st, a);
-    if (n == a.S) return;  // (no sequence of several pieces: nothing to join)
+    if (a.whole) return;  // (no sequence of several pieces: nothing to join)
     // the join: as few rows per workgroup (as many shares of the pieces) as fill the chip
     const int64_t R = static_cast<int64_t>(a.nq) * (a.heads / a.kv_heads), rows = std::min<int64_t>(R, p.rows);
     const int64_t joins = static_cast<int64_t>(a.S) * a.kv_heads * p.row_tiles, dims = d / 32;
@@ -1046,17 +1068,17 @@ hipError_t launch_paged_attention(hipStream_t st, PagedAttn a, int64_t d, bool f
     const dim3 jgrid(static_cast<unsigned>(joins), static_cast<unsigned>(dims * ((rows + a.join_rows - 1) / a.join_rows)));
     hipLaunchKernelGGL(join, jgrid, dim3(256), 0, st, a);
   };
-#define PA(D_, F_)                                                                                              \
-  if (p.rows == 128)                                                                                            \
-    launch(paged_attention_rows_kernel<D_, F_>, paged_join_kernel<D_, 128>, PagedTile<D_, F_, 2>::kKeys);       \
-  else if (p.rows == 32 && p.ways == 8)                                                                         \
-    launch(paged_attention_kernel<D_, F_, 2, 8>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys);       \
-  else if (p.rows == 32)                                                                                        \
-    launch(paged_attention_kernel<D_, F_, 2, 4>, paged_join_kernel<D_, 32>, PagedTile<D_, F_, 2>::kKeys);       \
-  else if (p.ways == 8)                                                                                         \
-    launch(paged_attention_kernel<D_, F_, 1, 8>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys);       \
-  else                                                                                                          \
-    launch(paged_attention_kernel<D_, F_, 1, 4>, paged_join_kernel<D_, 16>, PagedTile<D_, F_, 1>::kKeys);
+#define PA(D_, F_)                                                              \
+  if (p.rows == 128)                                                            \
+    launch(paged_attention_rows_kernel<D_, F_>, paged_join_kernel<D_, 128>);    \
+  else if (p.rows == 32 && p.ways == 8)                                         \
+    launch(paged_attention_kernel<D_, F_, 2, 8>, paged_join_kernel<D_, 32>);    \
+  else if (p.rows == 32)                                                        \
+    launch(paged_attention_kernel<D_, F_, 2, 4>, paged_join_kernel<D_, 32>);    \
+  else if (p.ways == 8)                                                         \
+    launch(paged_attention_kernel<D_, F_, 1, 8>, paged_join_kernel<D_, 16>);    \
+  else                                                                          \
+    launch(paged_attention_kernel<D_, F_, 1, 4>, paged_join_kernel<D_, 16>);
   if (d == 128 && fp8) {
     PA(128, true)
   } else if (d == 128) {

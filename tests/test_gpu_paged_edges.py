@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+import paper_2607_16339_amd as lc
 from paged_util import DEV, Cache, attend, normal
 
 pytestmark = pytest.mark.gpu
@@ -85,3 +86,45 @@ def test_values_of_hidden_keys_move_no_bit(length, key, nq, heads, kv, d, fp8):
         keep[0, sees, :, dim] = False
         assert torch.equal(_bits(o)[keep], _bits(want)[keep]), (dim, x)
         assert not bool(torch.isfinite(o.float())[~keep].any()), (dim, x)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,heads,kv", FORMS)
+def test_first_call_is_captured_where_no_sequence_can_be_cut(nq, heads, kv, d, fp8):
+    """A table of two tiles: the call needs no workspace, so the library need not have one."""
+    c = Cache([60, 1, 64], heads, kv, d, 16, fp8, seed=nq + d)
+    q = _q(c, nq)
+    o, lse = torch.empty_like(q), torch.empty(q.shape[:3], dtype=torch.float32, device=DEV)
+    torch.cuda.synchronize()
+    lc.lacache_release_workspace()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lc.lacache_paged_attention(q, c.k, c.v, c.table, c.lens, o, lse=lse, k_scale=c.k_scale, v_scale=c.v_scale,
+                                   causal=True)
+    want, wl = attend(c, q, True)
+    for _ in range(3):
+        o.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(_bits(o), _bits(want)) and torch.equal(_bits(lse), _bits(wl))
+
+
+def test_library_workspace_is_bounded_by_the_table():
+    """32 tokens of 32 heads over 8 KV heads and a table of 1024 keys: at most 16 pieces of 8 KV
+    heads with 128 rows, 8.5 MB, where tables without end would need 136."""
+    c = Cache([1000], 32, 8, 128, 16, False, seed=24, max_pages=64)
+    q = _q(c, 32)
+    o = torch.empty_like(q)
+    torch.cuda.synchronize()
+    lc.lacache_release_workspace()
+    free = torch.cuda.mem_get_info()[0]
+    lc.lacache_paged_attention(q, c.k, c.v, c.table, c.lens, o)
+    torch.cuda.synchronize()
+    taken = free - torch.cuda.mem_get_info()[0]
+    n = lc.lacache_paged_attention_workspace_bytes(1, 32, 32, 8, 128)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    want, _ = attend(c, q, False, workspace=ws)
+    torch.cuda.synchronize()
+    assert n > 100 << 20 and 0 < taken <= 16 << 20, (n, taken)
+    assert torch.equal(_bits(o), _bits(want))
