@@ -190,13 +190,14 @@ __device__ __forceinline__ void lin_frag(const uint8_t* rows, int lr, int q, bf8
 
 //
 // kRope: a slab is 8 pairs, rows i .. i + 7 of a head and then i + 64 .. i + 71;
-// kSwiGlu: rows n .. n + 7 and then N/2 + n .. (N: the weight rows).
+// kSwiGlu: rows n .. n + 7 and then N/2 + n .. (N: the weight rows). out may be the
+// residual of kAct and kSwiGlu: a thread reads an element before it stores it.
 template <int MT, int NJ, int kEpi>
 __global__ __launch_bounds__(kLinSplit * 64) void linear_bf16_kernel(const uint16_t* __restrict__ a,
                                                                      const uint16_t* __restrict__ w,
-                                                                     uint16_t* __restrict__ out,
-                                                                     float* __restrict__ out_tap, int64_t M,
-                                                                     int64_t N, int64_t K, EpiArgs<kEpi> ra) {
+                                                                     uint16_t* out, float* __restrict__ out_tap,
+                                                                     int64_t M, int64_t N, int64_t K,
+                                                                     EpiArgs<kEpi> ra) {
   using C = LinCfg<MT, NJ>;
   constexpr int D = C::D, RA = C::RA, NC = 16 * NJ;
   __shared__ __align__(16) uint8_t ring[kLinSplit][D * C::kSlot];
