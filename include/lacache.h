@@ -440,8 +440,9 @@ size_t lacache_first_layer_workspace_bytes(int64_t R, int64_t heads, int64_t H);
  * to 128 rows that are bound by reading w), or one chain over K, as the sizes
  * decide: a row's last bits may differ between calls of different M.
  *   NONE x; RELU max(x, 0); SILU x / (1 + e^-x); GELU x (1 + erf(x / sqrt 2)) / 2
- *   (off by at most 0.75e-7 |x| before the rounding); GELU_TANH x (1 +
- *   tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
+ *   (off by at most 8e-7 |x| before the rounding; of gelu(x) itself that is less than
+ *   a bf16 rounding down to x = -6 and 1 % at -8, where gelu(x) is -5e-15); GELU_TANH
+ *   x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
  *   SWIGLU: w is [2N x K], gate rows first, and bias [2N]: silu(a w_gate^T +
  *   b_gate) (a w_up^T + b_up), as the FFN's gate/up stage in 16 bits.
  * Other act values: LACACHE_ERR_INVALID_ARG. SWIGLU needs N K < 2^30

@@ -11,9 +11,11 @@ __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float silu(float x) { return x * fast_rcp(1.0f + exp_neg(x)); }
 // gelu(x) = x Phi(x), Phi(x) = erfc(-x / sqrt 2) / 2, with erfc(z), z >= 0, by formula
 // 7.1.26 of Abramowitz and Stegun (t = 1 / (1 + 0.3275911 z), t times a polynomial of
-// degree 4 in t, times exp(-z^2); off by at most 1.5e-7, so gelu by 0.75e-7 |x|): 13
-// instructions where the library's erfc takes several times that, and it is applied
-// to every output.
+// degree 4 in t, times exp(-z^2)): 13 instructions where the library's erfc takes several
+// times that, and it is applied to every output. The formula is off by at most 1.5e-7,
+// so gelu by 0.75e-7 |x|; its steps in fp32 add up to 6.9e-7 |x| (the polynomial's
+// partial sums and the reciprocal's error are as large as erfc). Found: 4.1e-7 |x|. In
+// the far negative tail the formula's relative error grows: 4e-3 of gelu(x) at x = -6.
 __device__ __forceinline__ float gelu(float x) {
   const float z = __builtin_fabsf(x) * 0.70710678118654752f;
   const float t = fast_rcp(__builtin_fmaf(0.3275911f, z, 1.0f));
