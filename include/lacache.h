@@ -445,8 +445,9 @@ size_t lacache_first_layer_workspace_bytes(int64_t R, int64_t heads, int64_t H);
  *   x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2;
  *   SWIGLU: w is [2N x K], gate rows first, and bias [2N]: silu(a w_gate^T +
  *   b_gate) (a w_up^T + b_up), as the FFN's gate/up stage in 16 bits.
- * Other act values: LACACHE_ERR_INVALID_ARG. SWIGLU needs N K < 2^30
- * (LACACHE_ERR_UNSUPPORTED otherwise). A NaN is stored as 0x7FC0. No workspace.
+ * Other act values: LACACHE_ERR_INVALID_ARG. SWIGLU needs N K < 2^30, and a launch
+ * must count less than 2^32 threads (outputs of about 256 GiB do not;
+ * LACACHE_ERR_UNSUPPORTED otherwise). A NaN is stored as 0x7FC0. No workspace.
  */
 enum {
   LACACHE_ACT_NONE = 0,

@@ -682,6 +682,7 @@ int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, 
   if (!apart(rng(out, ob), {rng(a, M * K * 2), rng(w, rows * K * 2), rng(bias, bias ? rows * 2 : 0),
                             rng(residual, residual && residual != out ? ob : 0)}))
     return LACACHE_ERR_INVALID_ARG;
+  if (!linear_act_launches(M, N, K, act)) return LACACHE_ERR_UNSUPPORTED;
   return hip_status(launch_linear_act(static_cast<hipStream_t>(stream), a, w, bias, residual, out, M, N, K, act));
 }
 

@@ -116,7 +116,9 @@ void linear_tile(int64_t M, int64_t N, int64_t K, int (&tile)[2]);
 // residual); act is a LACACHE_ACT_ value, SWIGLU with w [2N x K], bias [2N].
 hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
-// The tile of the call above: activation rows and weight rows of a workgroup.
+// Can the call above be launched (2^32 threads cannot)?
+bool linear_act_launches(int64_t M, int64_t N, int64_t K, int act);
+// Its tile: activation rows and weight rows of a workgroup.
 void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]);
 // The same on the weight-streaming kernel, for the few rows it takes.
 struct ActArgs;

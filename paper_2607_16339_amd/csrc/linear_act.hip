@@ -12,6 +12,7 @@
 // past the weight's rows fetch the last one and are not stored.
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 
 #include "activation.h"
 #include "device.h"
@@ -373,14 +374,15 @@ __global__ __launch_bounds__(512) void linear_act_pairs_kernel(LinCall c) {
 // wavefronts, M = 512: 43, 36, 33); 256 x 256 on 4 wavefronts of 128 x 128 took 288 us
 // where these take 218, on 16 of 64 x 64 the same, with 32x32x16 MFMAs 231.
 struct Shape {
-  int bm, bn, fit;
+  int bm, bn, waves, fit;
   double start, step, chip, shared;
 };
-constexpr Shape kShapes[7] = {{32, 64, 2, 0.739, 0.080, 0.078, 0.043},  {64, 64, 2, 1.117, 0.040, 0.114, 0.103},
-                              {64, 128, 1, 1.517, 0.174, 0.203, 0.0},   {128, 128, 1, 1.499, 0.342, 0.235, 0.0},
-                              {128, 256, 1, 0.832, 0.868, 0.302, 0.0},  // 16 wavefronts
-                              {128, 256, 1, 4.854, 0.638, 0.337, 0.0},  // 8 in pairs
-                              {256, 256, 1, 5.993, 1.301, 0.297, 0.0}};
+constexpr Shape kShapes[7] = {{32, 64, 4, 2, 0.739, 0.080, 0.078, 0.043},  {64, 64, 8, 2, 1.117, 0.040, 0.114, 0.103},
+                              {64, 128, 8, 1, 1.517, 0.174, 0.203, 0.0},   {128, 128, 16, 1, 1.499, 0.342, 0.235, 0.0},
+                              {128, 256, 16, 1, 0.832, 0.868, 0.302, 0.0},
+                              {128, 256, 8, 1, 4.854, 0.638, 0.337, 0.0},  // in pairs, a workgroup per CU, as
+                              {256, 256, 8, 1, 5.993, 1.301, 0.297, 0.0}};
+constexpr int kFirstPairs = 5;
 constexpr int kStream = -1;
 
 int best_shape(int64_t M, int64_t Nw, int64_t K) {
@@ -412,6 +414,7 @@ hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
   const dim3 all(static_cast<unsigned>(items)), round(static_cast<unsigned>(items < cus ? items : cus));
 #define LT(I_, WR_, WC_, S_)                                                                                             \
   case I_:                                                                                                               \
+    static_assert(WR_ * WC_ == kShapes[I_].waves, "wavefronts");                                                         \
     hipLaunchKernelGGL((linear_act_tile_kernel<kGlu, kShapes[I_].bm, kShapes[I_].bn, WR_, WC_, S_>), all,                \
                        dim3(64 * WR_ * WC_), 0, st, c);                                                                  \
     break
@@ -429,6 +432,16 @@ hipError_t launch_shape(hipStream_t st, LinCall c, int shape) {
 }
 
 }  // namespace
+
+// The threads of a launch are counted in 32 bits.
+bool linear_act_launches(int64_t M, int64_t N, int64_t K, int act) {
+  const int64_t Nw = act == LACACHE_ACT_SWIGLU ? 2 * N : N;
+  if (M * Nw < int64_t(1) << 32) return true;  // (a thread has at least 8 products)
+  const int shape = best_shape(M, Nw, K);
+  if (shape == kStream || shape >= kFirstPairs) return true;
+  const Shape& s = kShapes[shape];
+  return (M + s.bm - 1) / s.bm * ((Nw + s.bn - 1) / s.bn) * 64 * s.waves <= UINT32_MAX;
+}
 
 hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {

@@ -4,7 +4,7 @@ addresses that are never dereferenced (every call here is refused)."""
 
 import pytest
 
-from test_paged_abi import INVALID, L, _attn  # noqa: F401
+from test_paged_abi import INVALID, L, UNSUP, _attn, _linear  # noqa: F401
 
 
 @pytest.mark.parametrize("scale", [2.4e38, 3.0e38, 3.4e38])
@@ -12,3 +12,9 @@ def test_scale_whose_factor_in_base_2_is_infinite(L, scale):  # noqa: F811
     """A score of 0 times that factor would be no number. (2.4e38 log2(e) is above 3.4e38.)"""
     assert _attn(L, scale=scale) == INVALID
     assert _attn(L, S=0, scale=scale) == INVALID
+
+
+@pytest.mark.parametrize("sizes", [dict(M=1 << 24, N=8192), dict(M=1 << 24, N=131072), dict(M=1 << 24, N=4096, act=5)])
+def test_projection_whose_launch_would_count_too_many_threads(L, sizes):  # noqa: F811
+    """2^17 x 32 tiles of 128 x 256 on 16 wavefronts are 2^32 threads (the output, 256 GiB, fits the memory)."""
+    assert _linear(L, K=128, out=1 << 50, bias=None, residual=None, **sizes) == UNSUP
