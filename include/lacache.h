@@ -459,9 +459,10 @@ enum {
 };
 int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
-/* Test hook: the tile (activation rows, weight rows) that a workgroup of such a
- * call takes on the current device. M > 0. Launches nothing. */
+/* Test hooks: the tile (activation rows, weight rows) that a workgroup of such a
+ * call takes on the current device, and its wavefronts. M > 0. Launch nothing. */
 int lacache_linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile);
+int lacache_linear_act_waves(int64_t M, int64_t N, int64_t K, int act, int* waves);
 
 /*
  * Paged key/value cache: the keys and values of finished tokens (the prompt,

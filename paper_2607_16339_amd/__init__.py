@@ -448,6 +448,13 @@ def lacache_linear_act_tile(M, N, K, act=LACACHE_ACT_NONE):
     return tile[0], tile[1]
 
 
+def lacache_linear_act_waves(M, N, K, act=LACACHE_ACT_NONE):
+    """The wavefronts of a workgroup of lacache_linear_act_bf16 for a call of these sizes."""
+    waves = ctypes.c_int()
+    check(lib().lacache_linear_act_waves(M, N, K, act, ctypes.byref(waves)), "lacache_linear_act_waves")
+    return waves.value
+
+
 def lacache_status_string(status):
     return status_string(status)
 

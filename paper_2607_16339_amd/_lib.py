@@ -54,6 +54,7 @@ SIGNATURES = {
     "lacache_first_layer_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
     "lacache_linear_act_bf16": (_I, [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I]),
     "lacache_linear_act_tile": (_I, [_I64, _I64, _I64, _I, _P]),
+    "lacache_linear_act_waves": (_I, [_I64, _I64, _I64, _I, _P]),
     "lacache_paged_append": (_I, [_P, _P, _P, _P, _I64, _P, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _P, _P, _I64,
                                   _I64, _I64, _I64, _I64, _I]),
     "lacache_paged_attention": (_I, [_P] * 10 + [_I64] * 8 + [_F, _I, _I]),

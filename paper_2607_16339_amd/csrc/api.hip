@@ -268,6 +268,13 @@ int ffn_core(hipStream_t st, const uint16_t* x, const uint16_t* y, const uint16_
   return run_down(st, path, w.hq, w.hs, wd_q, wd_s, out, nullptr, M, H, I, w.scratch);
 }
 
+int check_linear_act(int64_t M, int64_t N, int64_t K, int act) {
+  if (act < LACACHE_ACT_NONE || act > LACACHE_ACT_SWIGLU) return LACACHE_ERR_INVALID_ARG;
+  RETURN_IF(check_m(M));
+  RETURN_IF(check_dim(N, kMaxN));
+  return check_dim(K, kMaxN);
+}
+
 // The sizes that the paged cache's calls share.
 constexpr int64_t kPagedMaxSeqs = 4096;
 constexpr int64_t kPagedMaxTokens = int64_t(1) << 22;  // of a sequence
@@ -668,10 +675,7 @@ int lacache_linear_bf16(void* stream, const uint16_t* a, const uint16_t* w, uint
 
 int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, const uint16_t* bias,
                             const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act) {
-  if (act < LACACHE_ACT_NONE || act > LACACHE_ACT_SWIGLU) return LACACHE_ERR_INVALID_ARG;
-  RETURN_IF(check_m(M));
-  RETURN_IF(check_dim(N, kMaxN));
-  RETURN_IF(check_dim(K, kMaxN));
+  RETURN_IF(check_linear_act(M, N, K, act));
   const bool glu = act == LACACHE_ACT_SWIGLU;
   const int64_t rows = glu ? 2 * N : N;
   // (the tiled kernel's 32-bit offsets into the pair rows)
@@ -687,14 +691,18 @@ int lacache_linear_act_bf16(void* stream, const uint16_t* a, const uint16_t* w, 
 }
 
 int lacache_linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile) {
-  if (act < LACACHE_ACT_NONE || act > LACACHE_ACT_SWIGLU) return LACACHE_ERR_INVALID_ARG;
-  RETURN_IF(check_m(M));
-  RETURN_IF(check_dim(N, kMaxN));
-  RETURN_IF(check_dim(K, kMaxN));
+  RETURN_IF(check_linear_act(M, N, K, act));
   if (M == 0 || tile == nullptr) return LACACHE_ERR_INVALID_ARG;
-  int t[2];
-  linear_act_tile(M, N, K, act, t);
-  std::memcpy(tile, t, sizeof(t));
+  int waves;
+  linear_act_tile(M, N, K, act, tile, &waves);
+  return LACACHE_OK;
+}
+
+int lacache_linear_act_waves(int64_t M, int64_t N, int64_t K, int act, int* waves) {
+  RETURN_IF(check_linear_act(M, N, K, act));
+  if (M == 0 || waves == nullptr) return LACACHE_ERR_INVALID_ARG;
+  int tile[2];
+  linear_act_tile(M, N, K, act, tile, waves);
   return LACACHE_OK;
 }
 

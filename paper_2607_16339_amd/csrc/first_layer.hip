@@ -168,7 +168,7 @@ __device__ __forceinline__ void quiet_stored(uint2* p) {
 // K-step (the lanes' chunks q and 4 + q). Several weight slabs per workgroup
 // share each staged activation row, so the activations (re-read from L2 by
 // every workgroup) cost less of the CU's copy bandwidth than the weights.
-constexpr int kLinSplit = 4;
+constexpr int kLinSplit = kStreamWaves;
 
 template <int MT, int NJ>
 struct LinCfg {

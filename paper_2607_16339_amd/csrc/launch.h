@@ -118,11 +118,12 @@ hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* 
                              const uint16_t* residual, uint16_t* out, int64_t M, int64_t N, int64_t K, int act);
 // Can the call above be launched (2^32 threads cannot)?
 bool linear_act_launches(int64_t M, int64_t N, int64_t K, int act);
-// Its tile: activation rows and weight rows of a workgroup.
-void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]);
+// Its tile, activation rows and weight rows of a workgroup, and the workgroup's wavefronts.
+void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile, int* waves);
 // The same on the weight-streaming kernel, for the few rows it takes.
 struct ActArgs;
 bool linear_streams_rows(int64_t M);
+constexpr int kStreamWaves = 4;
 hipError_t launch_linear_act_rows(hipStream_t st, const uint16_t* a, const uint16_t* w, const ActArgs& act, uint16_t* out,
                                   int64_t M, int64_t N, int64_t K);
 // q, k, v rows of RoPE(y w_qkv^T) (rows [R], w_qkv [3 heads 128 x H]): the

@@ -453,11 +453,15 @@ hipError_t launch_linear_act(hipStream_t st, const uint16_t* a, const uint16_t* 
   return glu ? launch_shape<true>(st, c, shape) : launch_shape<false>(st, c, shape);
 }
 
-void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int (&tile)[2]) {
+void linear_act_tile(int64_t M, int64_t N, int64_t K, int act, int* tile, int* waves) {
   const int64_t Nw = act == LACACHE_ACT_SWIGLU ? 2 * N : N;
   const int shape = best_shape(M, Nw, K);
-  if (shape == kStream) return linear_tile(M, Nw, K, tile);
-  tile[0] = kShapes[shape].bm, tile[1] = kShapes[shape].bn;
+  int t[2];
+  if (shape == kStream)
+    linear_tile(M, Nw, K, t), *waves = kStreamWaves;
+  else
+    t[0] = kShapes[shape].bm, t[1] = kShapes[shape].bn, *waves = kShapes[shape].waves;
+  tile[0] = t[0], tile[1] = t[1];
 }
 
 }  // namespace lacache
