@@ -533,7 +533,10 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
  * key (an empty sequence, a causal token before the first key), or whose scores
  * are all -inf, gets o = 0 and lse = -inf. What lies behind a sequence's end on
  * its last page, or a causal token's own place, does not reach the result,
- * whatever it holds. scale must not be negative, and scale log2(e) finite in fp32.
+ * whatever it holds. An infinity or a NaN among the values that a row sees makes
+ * its own dimension of that row's o infinite or NaN; one among the keys may make
+ * the whole row NaN.
+ * scale must not be negative, and scale log2(e) finite in fp32.
  * Arithmetic: exact products of bf16 (e4m3) values accumulated in fp32 (MFMA),
  * scales applied in fp32, softmax in base 2 in fp32, P to 16 bits (two bf16
  * terms) for the P V product, o rounded to bf16 once. A sequence's keys are

@@ -351,15 +351,17 @@ __global__ __launch_bounds__(512) void linear_act_pairs_kernel(LinCall c) {
   }
 }
 
-// The tiles, and what a call costs on each: rounds (of `fit` workgroups per CU) of a
+// The tiles, and a cost that ranks them: rounds (of `fit` workgroups per CU) of a
 // start and K/64 steps, a step's part in the traffic of the whole chip, and a part
-// for every workgroup that shares a CU. Up to 128 rows the weight-streaming kernel of
+// for every workgroup that shares a CU. (The constants are fitted to the order of the
+// times, not to the times: M = 32, N = K = 4096 costs 7.6 on the streaming kernel and 9.9
+// on 32 x 64 tiles.) Up to 128 rows the weight-streaming kernel of
 // the first layer (K over four wavefronts, 16 or 48 weight rows) competes. Weighed on
 // 376 sizes with weights from HBM, M = 1..8192, N x K = 128 x 4096 to 24576 x 4096, K
 // from 128 to 16384, all kernels in turn in one process: the choice is on average 0.2 %
 // slower than the best, 7 % at most (on 76 more, of other N and K, 0.9 % and 12 %);
 // without one of the two 128 x 256 tiles 1 % and 27 %, without 64 x 64 or 64 x 128 more.
-// In us on the streaming kernel, 32 x 64, 64 x 64, 64 x 128, 128 x 128, 128 x 256 (16
+// Times in us, weights from HBM, on the streaming kernel, 32 x 64, 64 x 64, 64 x 128, 128 x 128, 128 x 256 (16
 // wavefronts, 8 in pairs) and 256 x 256:
 //   N = K = 4096       M =   32  11, 17, 19, 27, 30, 67, 58, 80
 //                           128  24, 17, 21, 29, 38, 75, 59, 83

@@ -769,10 +769,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(PagedAt
 
 // More than 64 rows: four wavefronts of 32 rows each share every tile of keys, which
 // comes in stages of kTiles tiles (16 KB of keys, 16 of values) through two LDS
-// buffers, each wavefront copying its share; one barrier per stage. The products and
-// the softmax bound these calls, not the stream: the matrix cores are busy 30 % of the
-// time (P's second term counted), the vector units 50 % (256 rows over 8 sequences of
-// 4000 keys, 350 TFLOP/s), and two wavefronts per SIMD overlap little more than that.
+// buffers, each wavefront copying its share; one barrier per stage. The stream does not
+// bound these calls, nor is a unit full: the matrix cores are busy 30 % of the time (P's
+// second term counted), the vector units 50 % (256 rows over 8 sequences of 4000 keys,
+// 350 TFLOP/s); a wavefront's steps wait for each other, and two wavefronts per SIMD
+// overlap little more than that.
 // Against row tiles of 32 whose wavefronts split the keys (8 sequences of 1000..4096
 // keys, 8 KV heads, D = 128): 72 rows 35.7 us against 42.9, 96 37.8 / 43.7, 128 41.1 /
 // 46.1, 256 76 / 86; one sequence of 65536 and 96 rows 90 / 118; 64 sequences of 128
@@ -949,8 +950,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttn a) {
 // split the rows (the times of both stand at that kernel).
 // Where the wavefronts split the keys: one workgroup of 8 per CU while the sequences,
 // uncut, are too few for two of 4. Shorter runs per wavefront cost less than a cut
-// with its join: 8 blocks of 32 tokens, 700..1024 keys and 32 heads 25.6 us against
-// 30.6, 32 tokens with 200..1024 keys 17.8 / 22.9, 8 with 100..1000 12.2 / 14.4, 48
+// with its join (times of one state's calls in a row): 8 blocks of 32 tokens, 700..1024
+// keys and 32 heads 25.6 us against 30.6, 32 tokens with 200..1024 keys 17.8 / 22.9, 8 with 100..1000 12.2 / 14.4, 48
 // with 1..8191 154.7 / 156.6 (longer sequences that have to be cut are even, 1 to
 // 131072 keys, or lose to their longer pieces, 8 of 1000..4096 23.9 / 22.0). With more
 // sequences two workgroups of 4 per CU hide each other's start and end: 128 of
