@@ -539,7 +539,8 @@ int lacache_paged_append(void* stream, const uint16_t* qkv, const int32_t* seq_i
  * scale must not be negative, and scale log2(e) finite in fp32.
  * Arithmetic: exact products of bf16 (e4m3) values accumulated in fp32 (MFMA),
  * scales applied in fp32, softmax in base 2 in fp32, P to 16 bits (two bf16
- * terms) for the P V product, o rounded to bf16 once. A sequence's keys are
+ * terms) for the P V product, whose sums before the division (up to 2^8 times the
+ * sum of |v|) must stay within fp32, o rounded to bf16 once. A sequence's keys are
  * cut into pieces whose sums are joined; where the cuts lie depends on the lengths of
  * the call, so a row's last bits may differ between batches (the same inputs
  * give the same bytes). S == 0 launches nothing. Uses the library workspace
